@@ -1,7 +1,7 @@
-"""B200-native TAOT replica-placement planner: thin Python binding over libtaot.so.
+"""B200-native TAOT replica-placement planner and the layer operators around it: thin Python binding over libtaot.so.
 
 Every step of the path runs in the CUDA library; this package only marshals torch device
-tensors into the C ABI declared in include/taot.h.  There is no CPU fallback: importing the
+tensors into the C ABI declared in include/taot.h and include/taot_layer.h.  There is no CPU fallback: importing the
 binding without the compiled library raises.
 """
 from .binding import (  # noqa: F401
@@ -31,5 +31,17 @@ from .binding import (  # noqa: F401
     PipelinedHostPlanner,
     StreamingHostPlanner,
     split_layers,
+)
+from .layer import (  # noqa: F401
+    NormParams,
+    RouteParams,
+    RowsParams,
+    rms_norm,
+    rms_norm_backward,
+    route,
+    route_backward,
+    send,
+    combine,
+    combine_backward,
 )
 from .report import format_layer  # noqa: F401

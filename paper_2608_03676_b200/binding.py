@@ -28,6 +28,8 @@ _SYMBOLS = [
     "taot_histogram", "taot_histogram_static", "taot_excess_spare", "taot_sinkhorn", "taot_match", "taot_assign",
     "taot_plan", "taot_plan_host", "taot_host_block_layout", "taot_plan_host_block", "taot_report", "taot_dispatch", "taot_measure_alu_peaks", "taot_measure_latencies", "taot_measure_round_latencies", "taot_set_profiling", "taot_get_stage_ms", "taot_get_match_cycles", "taot_get_group_trace", "taot_tier_structure", "taot_last_launch_count",
     "taot_status_string",
+    "taot_rms_norm", "taot_rms_norm_backward", "taot_rms_norm_backward_workspace", "taot_route", "taot_route_backward",
+    "taot_send", "taot_combine", "taot_combine_backward",
 ]
 
 
