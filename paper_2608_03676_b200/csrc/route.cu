@@ -1,185 +1,24 @@
 // Routing of tokens to experts, and the gradient of the experts' weights (taot_layer.h).
-#include <cfloat>
-#include <cmath>
-
-#include "layer_common.cuh"
+#include "route_common.cuh"
 
 namespace {
 
 using namespace layer;
+using namespace route;
 
-constexpr int kMaxE = 1024;
-constexpr int kMaxK = 64;
-constexpr int kMaxGroups = 64;
 constexpr int kWarps = 4;                          // rows of a CTA, one per warp
-constexpr unsigned kAll = 0xffffffffu;
 
-struct RouteArgs {
-    const void* logits;
-    const float* bias;
-    const uint8_t* mask;
-    int32_t* topk;
-    float* weights;
-    int64_t N, T, ld;
-    float scale;
-    int32_t E, k, score, groups, kept, top, renormalise, dtype;
-};
-
-// A logit as every kernel here sees it: -infinity if the expert is closed, an infinite one as the largest finite value of the type
-__device__ __forceinline__ float logit_at(const void* p, int64_t i, int32_t dtype)
-{
-    float v, big;
-    if (dtype == TAOT_F32) { v = static_cast<const float*>(p)[i]; big = FLT_MAX; }
-    else if (dtype == TAOT_BF16) { v = to_f32(static_cast<const __nv_bfloat16*>(p)[i]); big = 3.38953139e38f; }
-    else { v = to_f32(static_cast<const __half*>(p)[i]); big = 65504.0f; }
-    return v > -big ? fminf(v, big) : -INFINITY;   // (false for a NaN)
-}
-
-// (down to the smallest values: the exponential is that of a number that is not positive)
-__device__ __forceinline__ float sigmoid(float x)
-{
-    const float e = expf(-fabsf(x));
-    return (x < 0.0f ? e : 1.0f) / (1.0f + e);
-}
-
-__device__ __forceinline__ double warp_max(double v)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmax(v, __shfl_xor_sync(kAll, v, o));
-    return v;
-}
-__device__ __forceinline__ float warp_max(float v)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
-    return v;
-}
-
-// the largest value of a warp and the lowest index that has it
-__device__ __forceinline__ void warp_argmax(double& v, int& i)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const double u = __shfl_xor_sync(kAll, v, o);
-        const int j = __shfl_xor_sync(kAll, i, o);
-        if (u > v || (u == v && j < i)) { v = u; i = j; }
-    }
-}
-
-// The chosen experts of one row, by arithmetic in 64 bits: lane j % 32 holds place j in at[j / 32], -1 where no expert is left.
-// key [E] is shared memory of the warp.  top and total: the largest open logit and the sum of exp(logit - top).
-__device__ void choose_exactly(const RouteArgs& a, int64_t row, double* key, int (&at)[2], double& top, double& total)
-{
-    const int lane = threadIdx.x & 31;
-    const float* bias = a.bias ? a.bias + row / a.T * a.E : nullptr;
-    top = -INFINITY;
-    for (int e = lane; e < a.E; e += 32) {
-        const double x = logit_at(a.logits, row * a.ld + e, a.dtype);
-        key[e] = x;
-        top = fmax(top, x);
-    }
-    top = warp_max(top);
-    total = 0.0;
-    if (a.score == TAOT_SOFTMAX && top > -INFINITY) {
-        for (int e = lane; e < a.E; e += 32) total += exp(key[e] - top);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
-    }
-    if (bias || a.groups > 1)
-        for (int e = lane; e < a.E; e += 32) {
-            const double x = key[e], b = bias ? (double)bias[e] : 0.0;
-            const double s = a.score == TAOT_SOFTMAX ? exp(x - top) / total : 1.0 / (1.0 + exp(-x));
-            key[e] = x > -INFINITY && isfinite(b) ? s + b : -INFINITY;
-        }
-    __syncwarp();
-    if (a.groups > 1) {
-        const int size = a.E / a.groups;
-        double score[2] = {-INFINITY, -INFINITY};
-        for (int h = 0; h < 2; ++h) {
-            const int g = lane + 32 * h;
-            if (g >= a.groups) continue;
-            double m1 = -INFINITY, m2 = -INFINITY;
-            for (int e = g * size; e < (g + 1) * size; ++e) {
-                const double v = key[e];
-                if (v > m1) { m2 = m1; m1 = v; }
-                else if (v > m2) m2 = v;
-            }
-            score[h] = a.top == 2 && m2 > -INFINITY ? m1 + m2 : m1;
-        }
-        bool in[2] = {false, false};
-        bool left[2] = {lane < a.groups, lane + 32 < a.groups};
-        for (int i = 0; i < a.kept; ++i) {
-            double v = -INFINITY;
-            int g = kMaxGroups;
-            for (int h = 1; h >= 0; --h)
-                if (left[h] && score[h] >= v) { v = score[h]; g = lane + 32 * h; }
-            warp_argmax(v, g);
-            for (int h = 0; h < 2; ++h)
-                if (g == lane + 32 * h) { in[h] = true; left[h] = false; }
-        }
-        const uint64_t kept = (uint64_t)__ballot_sync(kAll, in[0]) | (uint64_t)__ballot_sync(kAll, in[1]) << 32;
-        for (int e = lane; e < a.E; e += 32) {
-            const bool in_group = (kept >> (e / size)) & 1;
-            if (!in_group) key[e] = -INFINITY;
-            else if (!bias) key[e] = logit_at(a.logits, row * a.ld + e, a.dtype);
-        }
-        __syncwarp();
-    }
-    at[0] = at[1] = -1;
-    for (int j = 0; j < a.k; ++j) {
-        double v = -INFINITY;
-        int i = kMaxE;
-        for (int e = lane; e < a.E; e += 32)
-            if (key[e] > v) { v = key[e]; i = e; }
-        warp_argmax(v, i);
-        if (v == -INFINITY) break;                 // (the same for all lanes)
-        if ((j & 31) == lane) at[j >> 5] = i;
-        if (lane == 0) key[i] = -INFINITY;
-        __syncwarp();
-    }
-}
-
-// Writes a row's table entries and weights: lane j % 32 holds place j in at[j / 32].
-__device__ __forceinline__ void write_row(const RouteArgs& a, int64_t row, const int (&at)[2], float top, float total)
-{
-    const int lane = threadIdx.x & 31;
-    float x[2], w[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) x[h] = at[h] >= 0 ? logit_at(a.logits, row * a.ld + at[h], a.dtype) : -INFINITY;
-    if (a.renormalise) {
-        // relative to the largest chosen score, where the scores would leave the range of fp32 (below -40, where
-        // 1 / (1 + exp(-x)) is exp(x) to 18 digits) or are a softmax
-        const float most = warp_max(fmaxf(x[0], x[1]));
-        const bool shift = a.score == TAOT_SOFTMAX || most < -40.0f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) w[h] = at[h] < 0 ? 0.0f : shift ? expf(x[h] - most) : sigmoid(x[h]);
-        const float sum = warp_sum(w[0] + w[1]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) w[h] = at[h] < 0 ? 0.0f : w[h] / sum;
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) w[h] = at[h] < 0 ? 0.0f : a.score == TAOT_SOFTMAX ? expf(x[h] - top) / total : sigmoid(x[h]);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int j = lane + 32 * h;
-        if (j < a.k) {
-            a.topk[row * a.k + j] = at[h];
-            if (a.weights) a.weights[row * a.k + j] = a.scale * w[h];
-        }
-    }
-}
-
+// One warp per row, in 64 bits throughout: more than 16 places, or groups that the other kernels are not made for.
 __global__ void __launch_bounds__(kWarps * 32)
-route_kernel(RouteArgs a)
+route_kernel(const __grid_constant__ RouteArgs a)
 {
     extern __shared__ double keys[];
     const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (row >= a.N) return;
-    int at[2] = {-1, -1};
-    double top = 0.0, total = 1.0;
-    if (!a.mask || a.mask[row]) choose_exactly(a, row, keys + (threadIdx.x >> 5) * a.E, at, top, total);
-    write_row(a, row, at, (float)top, (float)total);
+    int at0 = -1, at1 = -1;
+    float top = 0.0f, total = 1.0f;
+    if (!a.mask || a.mask[row]) choose_exactly(a, row, keys + (threadIdx.x >> 5) * a.E, at0, at1, top, total);
+    write_row(a, row, at0, at1, top, total);
 }
 
 struct RouteGradArgs {
@@ -311,8 +150,16 @@ extern "C" int taot_route(const taot_route_params* p, const void* d_logits, cons
     a.N = N; a.T = p->T; a.ld = p->ld_logits; a.scale = p->scale;
     a.E = p->E; a.k = p->k; a.score = p->score; a.groups = p->groups; a.kept = p->groups_kept; a.top = p->group_top;
     a.renormalise = p->renormalise; a.dtype = p->dtype;
-    route_kernel<<<(unsigned)((N + kWarps - 1) / kWarps), kWarps * 32, sizeof(double) * kWarps * p->E, static_cast<cudaStream_t>(stream)>>>(a);
-    TAOT_CUDA_OK(cudaGetLastError());
+    a.chunk_bits = 1;
+    while ((1 << a.chunk_bits) <= (p->E + 3) / 4) ++a.chunk_bits;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool lists = p->k <= 16 && (p->groups == 1 || ((p->groups == 2 || p->groups == 4 || p->groups == 8) && p->E % 32 == 0));
+    if (lists) {
+        TAOT_CUDA_OK(launch_lanes(a, wide_rows(d_logits, p->ld_logits, e), st));
+    } else {
+        route_kernel<<<(unsigned)((N + kWarps - 1) / kWarps), kWarps * 32, sizeof(double) * kWarps * p->E, st>>>(a);
+        TAOT_CUDA_OK(cudaGetLastError());
+    }
     return TAOT_OK;
 }
 

@@ -1,0 +1,393 @@
+// Routing with eight lanes per row: calls of few rows, whose time is that of one row (route_common.cuh: how the choice is made).
+#include "route_common.cuh"
+
+namespace route {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kLanes = 8;
+constexpr int kRows = 32 / kLanes;                 // of a warp
+
+__device__ __forceinline__ float row_max(float v)
+{
+#pragma unroll
+    for (int o = 1; o < kLanes; o *= 2) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
+    return v;
+}
+__device__ __forceinline__ float row_min(float v) { return -row_max(-v); }
+__device__ __forceinline__ float row_sum(float v)
+{
+#pragma unroll
+    for (int o = 1; o < kLanes; o *= 2) v += __shfl_xor_sync(kAll, v, o);
+    return v;
+}
+
+// merges the lists of the eight lanes of a row; all lanes end with the same list
+template <bool LOST, int K>
+__device__ __forceinline__ void merge_lanes(uint32_t (&v)[K], uint32_t& lost)
+{
+#pragma unroll
+    for (int o = 1; o < kLanes; o *= 2) {
+        uint32_t w[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) w[i] = __shfl_xor_sync(kAll, v[i], o);
+        if (LOST) lost = max(lost, __shfl_xor_sync(kAll, lost, o));
+        merge_list<LOST>(v, w, lost);
+    }
+}
+
+// the four logits of chunk c, NaN beyond the last expert
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load_chunk(const T* row, int c, int E, float (&x)[4])
+{
+    if (WIDE) four(row + 4 * c, x);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = 4 * c + i < E ? to_f32(row[4 * c + i]) : __int_as_float(0x7fc00000);
+}
+
+// BIAS: keys are scores with a bias added.  GROUP: 2, 4 or 8 groups; a lane's chunks follow one another, so that a group lies in
+// 4, 2 or 1 lanes (E is a multiple of 32).  WIDE: rows of whole chunks that can be read as such.  U: chunks of a lane that
+// are taken at a time (4 where it has no more).
+template <typename T, int K, int U, bool BIAS, bool GROUP, bool WIDE>
+__global__ void __launch_bounds__(kWarps * 32)
+route_lanes_kernel(const __grid_constant__ RouteArgs a)
+{
+    extern __shared__ double keys[];
+    constexpr int kOwn = K / kLanes;                               // places of the list that a lane stands for
+    constexpr uint32_t kSlots = 4 * K - 1;
+    constexpr bool kExact = !BIAS && sizeof(T) == 2;               // keys lose nothing
+    constexpr uint32_t kLow = 0x1fff;                              // bits that the fp32 form of a 16-bit number leaves
+    constexpr float big = Type<T>::big;
+    const int lane = threadIdx.x & 31, sub = lane & (kLanes - 1);
+    const int64_t first = ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kRows;
+    if (first >= a.N) return;
+    const int64_t mine = first + lane / kLanes;
+    const int64_t row = mine < a.N ? mine : a.N - 1;               // (lanes past the end repeat the last row and write nothing)
+    const bool routed = mine < a.N && (!a.mask || a.mask[row]);
+    const T* x_row = static_cast<const T*>(a.logits) + row * a.ld;
+    const float* b_row = BIAS ? a.bias + row / a.T * a.E : nullptr;
+    const int C = (a.E + 3) / 4;
+    const int per = (C + kLanes - 1) / kLanes;                     // chunks of a lane
+    const uint32_t cmask = (1u << a.chunk_bits) - 1;
+    const uint32_t drop = max(cmask, kSlots);                      // the bits of a key that are no value
+
+    Scores sc = {0.0f, 1.0f};
+    float total = 1.0f;
+    if (a.score == TAOT_SOFTMAX && (BIAS || GROUP || (!a.renormalise && a.weights))) {
+        float top = -big;
+        for (int c = sub; c < C; c += kLanes) {
+            float x[4];
+            load_chunk<T, WIDE>(x_row, c, a.E, x);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) top = fmaxf(top, x[q]);
+        }
+        sc.top = top = fminf(row_max(top), big);
+        total = 0.0f;
+        for (int c = sub; c < C; c += kLanes) {
+            float x[4];
+            load_chunk<T, WIDE>(x_row, c, a.E, x);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) total += x[q] > -big ? fast_exp2((fminf(x[q], big) - top) * kLog2e) : 0.0f;
+        }
+        total = row_sum(total);
+        sc.inv = 1.0f / total;
+    }
+    const float off = score_error(a.score, sc, (a.E + kLanes - 1) / kLanes);
+
+    // the K best chunks
+    uint32_t best[K], lost = 0, bits = 0;
+    float g1 = -INFINITY, g2 = -INFINITY;                          // the two largest keys of the lane's part of its group
+    for (int i0 = 0; i0 < per; i0 += U) {
+        uint32_t list[K];
+#pragma unroll
+        for (int u = 0; u < K; ++u) list[u] = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u;
+            const int c = GROUP ? sub * per + i : i * kLanes + sub;
+            if (i >= per || c >= C) continue;
+            float x[4], m = -INFINITY;
+            load_chunk<T, WIDE>(x_row, c, a.E, x);
+            if (BIAS) {
+                float b[4];
+                if (WIDE) four(b_row + 4 * c, b);
+                else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) b[q] = 4 * c + q < a.E ? b_row[4 * c + q] : INFINITY;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    x[q] = x[q] > -big && fabsf(b[q]) < INFINITY ? score_of(a.score, sc, fminf(x[q], big)) + b[q] : -INFINITY;
+            } else if (GROUP || !kExact) {
+                if (!kExact) bits |= __float_as_uint(x[0]) | __float_as_uint(x[1]) | __float_as_uint(x[2]) | __float_as_uint(x[3]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = seen(x[q], big);
+            }
+            if (GROUP) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    g2 = fmaxf(g2, fminf(g1, x[q]));
+                    g1 = fmaxf(g1, x[q]);
+                }
+            }
+            m = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+            m = seen(m, big) + 0.0f;                               // (+ 0: one zero)
+            list[u] = m > -INFINITY ? (ordered(m) & ~cmask) | (cmask - (uint32_t)c) : 0u;
+        }
+        sort_list(list);
+        if (i0 == 0) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) best[i] = list[i];
+        } else {
+            merge_list<!kExact>(best, list, lost);
+        }
+    }
+    bool redo = false;
+    if (GROUP) {
+        const int lanes = kLanes / a.groups;                       // of a group
+        for (int o = 1; o < lanes; o *= 2) {
+            const float h1 = __shfl_xor_sync(kAll, g1, o), h2 = __shfl_xor_sync(kAll, g2, o);
+            g2 = fmaxf(fminf(g1, h1), fmaxf(g2, h2));
+            g1 = fmaxf(g1, h1);
+        }
+        float s1 = g1, s2 = g2;
+        if (!BIAS) {
+            s1 = g1 > -INFINITY ? score_of(a.score, sc, g1) : -INFINITY;
+            s2 = g2 > -INFINITY ? score_of(a.score, sc, g2) : -INFINITY;
+        }
+        const float score = a.top == 2 && s2 > -INFINITY ? s1 + s2 : s1;
+        const int g = sub / lanes;
+        int rank = 0;
+#pragma unroll
+        for (int o = 1; o < kLanes; ++o) {
+            const float other = __shfl_xor_sync(kAll, score, o);
+            const int h = (sub ^ o) / lanes;
+            if (h != g && (sub ^ o) % lanes == 0 && (other > score || (other == score && h < g))) ++rank;
+        }
+        const bool kept = rank < a.kept;
+        const float worst = row_min(kept ? score : INFINITY), next = row_max(kept ? -INFINITY : score);
+        const float size = row_max(s1 > -INFINITY ? fmaxf(fabsf(s1), s2 > -INFINITY ? fabsf(s2) : 0.0f) : 0.0f);
+        redo = a.kept < a.groups && !(worst - next > 4.0f * off + 8.0f * size * 1.2e-7f);
+        if (!kept) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) best[i] = 0;
+            lost = 0;
+        }
+    }
+    merge_lanes<!kExact>(best, lost);
+
+    // their experts: a lane takes chunks sub, sub + 8
+    int id[kOwn];
+    if (kExact) {
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (i % kLanes == sub) id[i / kLanes] = (int)(cmask - (best[i] & cmask));    // (none: cmask, which is behind all chunks)
+    } else {
+        uint32_t ids[K];                                           // in ascending order, so that places are in the experts' order
+#pragma unroll
+        for (int i = 0; i < K; ++i) ids[i] = ~(cmask - (best[i] & cmask));
+        sort_list(ids);
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (i % kLanes == sub) id[i / kLanes] = (int)~ids[i];
+    }
+    uint32_t list[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) list[i] = 0;
+#pragma unroll
+    for (int h = 0; h < kOwn; ++h) {
+        if (id[h] >= C) continue;
+        float x[4];
+        load_chunk<T, WIDE>(x_row, id[h], a.E, x);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = 4 * id[h] + q;
+            float v = seen(x[q], big) + 0.0f;
+            if (BIAS) {
+                const float b = WIDE || e < a.E ? b_row[e] : INFINITY;
+                v = v > -INFINITY && fabsf(b) < INFINITY ? score_of(a.score, sc, v) + b : -INFINITY;
+            }
+            const uint32_t low = kExact ? kLow - (uint32_t)e : kSlots - (uint32_t)(4 * (sub + kLanes * h) + q);
+            list[4 * h + q] = v > -INFINITY ? (ordered(v) & ~(kExact ? kLow : kSlots)) | low : 0u;
+        }
+    }
+    sort_list(list);
+    merge_lanes<!kExact>(list, lost);
+
+    // a lane's places
+    int at[kOwn];
+    float x[kOwn], v[kOwn];
+#pragma unroll
+    for (int h = 0; h < kOwn; ++h) {
+        uint32_t key = 0;
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (i == sub + kLanes * h) key = list[i];
+        const bool there = key != 0 && sub + kLanes * h < a.k;
+        if (kExact) {
+            at[h] = there ? (int)(kLow - (key & kLow)) : -1;
+        } else {
+            const int slot = (int)(kSlots - (key & kSlots));
+            const int from = (lane & ~(kLanes - 1)) | ((slot >> 2) & (kLanes - 1));
+            int chunk = __shfl_sync(kAll, id[0], from);
+            if constexpr (kOwn > 1) {
+                const int other = __shfl_sync(kAll, id[1], from);
+                if (slot >> 5) chunk = other;
+            }
+            at[h] = there ? 4 * chunk + (slot & 3) : -1;
+        }
+        x[h] = there ? seen(to_f32(x_row[at[h]]), big) : -INFINITY;
+        v[h] = x[h];
+    }
+    if (!kExact) {
+        // Is what was left out far enough below the last chosen one (the k-th, or the last there is)?  And are neighbours in order?
+        uint32_t beyond = lost, last = 0;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            if (i >= a.k) beyond = max(beyond, list[i]);
+            else last = list[i];
+        }
+        const bool lossless = !BIAS && (__reduce_or_sync(kAll, bits) & drop) == 0;
+        bool fine = true;                                          // this lane's places and their successors
+        if (BIAS) {
+            float b[kOwn];
+#pragma unroll
+            for (int h = 0; h < kOwn; ++h) {
+                b[h] = at[h] >= 0 ? b_row[at[h]] : 0.0f;
+                v[h] = at[h] >= 0 ? score_of(a.score, sc, x[h]) + b[h] : -INFINITY;
+            }
+            const float size = row_max(fmaxf(v[0] > -INFINITY ? fabsf(v[0]) : 0.0f, v[kOwn - 1] > -INFINITY ? fabsf(v[kOwn - 1]) : 0.0f));
+            const float err = 2.0f * off + 2.4e-7f * size;
+            if (K == 8) {                                          // put right what the lost bits have turned round
+                const float after = __shfl_down_sync(kAll, v[0], 1);
+                const int e_after = __shfl_down_sync(kAll, at[0], 1);
+                const bool turned = sub < kLanes - 1 && e_after >= 0 && (after > v[0] || (after == v[0] && e_after < at[0]));
+                if (__any_sync(kAll, turned)) {
+                    int rank = 0;
+#pragma unroll
+                    for (int o = 1; o < kLanes; ++o) {
+                        const float u = __shfl_xor_sync(kAll, v[0], o);
+                        const int e = __shfl_xor_sync(kAll, at[0], o);
+                        if (u > v[0] || (u == v[0] && ((e < at[0] && e >= 0) || (e == at[0] && (sub ^ o) < sub)))) ++rank;
+                    }
+                    int from = 0;                                  // the lane that has place sub
+#pragma unroll
+                    for (int o = 0; o < kLanes; ++o)
+                        if (__shfl_sync(kAll, rank, (lane & ~(kLanes - 1)) + o) == sub) from = o;
+                    from += lane & ~(kLanes - 1);
+                    at[0] = __shfl_sync(kAll, at[0], from);
+                    x[0] = __shfl_sync(kAll, x[0], from);
+                    v[0] = __shfl_sync(kAll, v[0], from);
+                    b[0] = __shfl_sync(kAll, b[0], from);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < kOwn; ++h) {
+                // the next place: the next lane's, or the next list's first
+                const int from = (lane & ~(kLanes - 1)) | ((sub + 1) & (kLanes - 1));
+                const bool wraps = sub == kLanes - 1;
+                float u = __shfl_sync(kAll, v[h], from), y = __shfl_sync(kAll, x[h], from), c = __shfl_sync(kAll, b[h], from);
+                int e = __shfl_sync(kAll, at[h], from);
+                if constexpr (kOwn > 1) {
+                    const float u1 = __shfl_sync(kAll, v[1], from), y1 = __shfl_sync(kAll, x[1], from), c1 = __shfl_sync(kAll, b[1], from);
+                    const int e1 = __shfl_sync(kAll, at[1], from);
+                    if (wraps && h == 0) { u = u1; y = y1; c = c1; e = e1; }
+                }
+                if (wraps && h == kOwn - 1) e = -1;
+                if (e >= 0 && !(v[h] - u > err) && !(x[h] == y && b[h] == c && at[h] < e)) fine = false;
+            }
+            const float least = row_min(fminf(v[0] > -INFINITY ? v[0] : INFINITY, v[kOwn - 1] > -INFINITY ? v[kOwn - 1] : INFINITY));
+            if (beyond != 0 && !(least > number_of(beyond | drop) + err)) fine = false;
+        } else if (!lossless) {
+            if (beyond != 0 && ((beyond ^ last) & ~drop) == 0) fine = false;
+            if (K == 8) {
+                const float after = __shfl_down_sync(kAll, x[0], 1);
+                if (sub < kLanes - 1 && after > x[0]) fine = false;
+            } else {
+#pragma unroll
+                for (int i = 0; i + 1 < K; ++i)
+                    if (i + 1 < a.k && list[i + 1] != 0 && ((list[i] ^ list[i + 1]) & ~drop) == 0) fine = false;
+            }
+        }
+        const unsigned bad = __ballot_sync(kAll, !fine);
+        redo = redo || ((bad >> (lane & ~(kLanes - 1))) & ((1u << kLanes) - 1)) != 0;
+    }
+    redo = redo && routed;
+    if (!routed) {
+#pragma unroll
+        for (int h = 0; h < kOwn; ++h) { at[h] = -1; x[h] = -INFINITY; }
+    }
+    float w[kOwn];
+    if (a.weights) {
+        float most = -INFINITY;
+        if (a.renormalise) most = row_max(fmaxf(x[0], x[kOwn - 1]));
+        const bool shift = a.renormalise && (a.score == TAOT_SOFTMAX || most < -40.0f);
+        float sum = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kOwn; ++h) {
+            w[h] = at[h] < 0 ? 0.0f : shift ? expf(x[h] - most) : a.score == TAOT_SIGMOID ? sigmoid(x[h]) : expf(x[h] - sc.top) * sc.inv;
+            sum += w[h];
+        }
+        if (a.renormalise) {
+            sum = row_sum(sum);
+            const float share = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+            for (int h = 0; h < kOwn; ++h) w[h] *= share;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < kOwn; ++h)
+        if (mine < a.N && !redo && sub + kLanes * h < a.k) {
+            a.topk[row * a.k + sub + kLanes * h] = at[h];
+            if (a.weights) a.weights[row * a.k + sub + kLanes * h] = a.scale * w[h];
+        }
+    if (BIAS || GROUP || !kExact) {
+        unsigned again = __ballot_sync(kAll, redo);
+        while (again) {
+            const int from = __ffs(again) - 1;
+            again &= ~(((1u << kLanes) - 1) << (from & ~(kLanes - 1)));
+            const int64_t r = first + from / kLanes;
+            int at0, at1;
+            float t, z;
+            choose_exactly(a, r, keys + (threadIdx.x >> 5) * a.E, at0, at1, t, z);
+            write_row(a, r, at0, at1, t, z);
+        }
+    }
+}
+
+template <typename T, int K, int U, bool WIDE>
+cudaError_t launch(const RouteArgs& a, cudaStream_t st)
+{
+    const unsigned grid = (unsigned)((a.N + kWarps * kRows - 1) / (kWarps * kRows));
+    const size_t scratch = sizeof(double) * kWarps * a.E;
+    if (a.groups > 1) {
+        if (a.bias) route_lanes_kernel<T, K, U, true, true, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
+        else route_lanes_kernel<T, K, U, false, true, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
+    } else {
+        if (a.bias) route_lanes_kernel<T, K, U, true, false, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
+        else route_lanes_kernel<T, K, U, false, false, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
+    }
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t by_shape(const RouteArgs& a, bool wide, cudaStream_t st)
+{
+    if (a.k > 8) return wide ? launch<T, 16, 8, true>(a, st) : launch<T, 16, 8, false>(a, st);
+    if (wide) return a.E <= 128 ? launch<T, 8, 4, true>(a, st) : launch<T, 8, 8, true>(a, st);
+    return launch<T, 8, 8, false>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_lanes(const RouteArgs& a, bool wide, cudaStream_t st)
+{
+    wide = wide && a.E % 4 == 0 && !misaligned(a.bias, 16);
+    if (a.dtype == TAOT_F32) return by_shape<float>(a, wide, st);
+    if (a.dtype == TAOT_BF16) return by_shape<__nv_bfloat16>(a, wide, st);
+    return by_shape<__half>(a, wide, st);
+}
+
+}  // namespace route
