@@ -12,7 +12,7 @@ constexpr int kWarps = 4;                          // rows of a CTA, one per war
 __global__ void __launch_bounds__(kWarps * 32)
 route_kernel(const __grid_constant__ RouteArgs a)
 {
-    extern __shared__ double keys[];
+    extern __shared__ uint64_t keys[];
     const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (row >= a.N) return;
     int at0 = -1, at1 = -1;
@@ -157,7 +157,7 @@ extern "C" int taot_route(const taot_route_params* p, const void* d_logits, cons
     if (lists) {
         TAOT_CUDA_OK(launch_lanes(a, wide_rows(d_logits, p->ld_logits, e), st));
     } else {
-        route_kernel<<<(unsigned)((N + kWarps - 1) / kWarps), kWarps * 32, sizeof(double) * kWarps * p->E, st>>>(a);
+        route_kernel<<<(unsigned)((N + kWarps - 1) / kWarps), kWarps * 32, sizeof(uint64_t) * kWarps * p->E, st>>>(a);
         TAOT_CUDA_OK(cudaGetLastError());
     }
     return TAOT_OK;

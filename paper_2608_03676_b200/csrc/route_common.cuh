@@ -48,12 +48,6 @@ __device__ __forceinline__ float sigmoid(float x)
     return __fdividef(x < 0.0f ? e : 1.0f, 1.0f + e);
 }
 
-__device__ __forceinline__ double warp_max(double v)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmax(v, __shfl_xor_sync(kAll, v, o));
-    return v;
-}
 __device__ __forceinline__ float warp_max(float v)
 {
 #pragma unroll
@@ -61,77 +55,178 @@ __device__ __forceinline__ float warp_max(float v)
     return v;
 }
 
-// the lowest index among the lanes' that has the largest value (kMaxE if that is -infinity)
-__device__ __forceinline__ int warp_argmax(double v, int i)
+// e^x in 64 bits, to about an ulp: x = n ln 2 + r with ln 2 in two parts (Cody and Waite), the Taylor series of e^r (|r| <= ln 2 / 2: its 14th term is
+// below 5e-18), and 2^n in two factors, so that results below 2^-1022 are rounded once.  No branches: several run side by side.
+__device__ __forceinline__ double exp_of(double x)
 {
-    const long long b = __double_as_longlong(v + 0.0);                       // one zero
-    const unsigned long long u = (unsigned long long)b ^ (b < 0 ? ~0ull : 1ull << 63);
+    x = fmin(fmax(x, -750.0), 750.0);                              // 0 and infinity beyond
+    const double whole = 6755399441055744.0;                       // 1.5 * 2^52: what is added to it is rounded to whole numbers
+    const double t = fma(x, 1.4426950408889634, whole);
+    const int n = __double2loint(t);
+    const double nd = t - whole;
+    double r = fma(nd, -6.93147180369123816490e-01, x);            // (the upper 33 bits of ln 2: the product is exact)
+    r = fma(nd, -1.90821492927058770002e-10, r);
+    double p = 1.0 / 6227020800.0;                                 // 1 / 13!
+    p = fma(p, r, 1.0 / 479001600.0);
+    p = fma(p, r, 1.0 / 39916800.0);
+    p = fma(p, r, 1.0 / 3628800.0);
+    p = fma(p, r, 1.0 / 362880.0);
+    p = fma(p, r, 1.0 / 40320.0);
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    const int half = n >> 1;
+    return p * __hiloint2double((half + 1023) << 20, 0) * __hiloint2double((n - half + 1023) << 20, 0);
+}
+
+// the order-preserving image of a number in 64 bits; closed experts (-infinity) have 0
+__device__ __forceinline__ uint64_t ordered(double v)
+{
+    const long long b = __double_as_longlong(v + 0.0);             // (one zero)
+    return v > -INFINITY ? (uint64_t)(b ^ ((b >> 63) | (long long)0x8000000000000000ull)) : 0ull;
+}
+__device__ __forceinline__ double number_of(uint64_t u)
+{
+    const long long b = (long long)u;
+    return u ? __longlong_as_double(b ^ (~(b >> 63) | (long long)0x8000000000000000ull)) : -INFINITY;
+}
+
+// the lowest index among the lanes' that has the largest key (kMaxE if that is 0)
+__device__ __forceinline__ int warp_argmax(uint64_t u, int i)
+{
     const uint32_t hi = (uint32_t)(u >> 32), most_hi = __reduce_max_sync(kAll, hi);
     const uint32_t lo = hi == most_hi ? (uint32_t)u : 0u, most_lo = __reduce_max_sync(kAll, lo);
-    return (int)__reduce_min_sync(kAll, hi == most_hi && (uint32_t)u == most_lo && v > -INFINITY ? (unsigned)i : (unsigned)kMaxE);
+    return (int)__reduce_min_sync(kAll, hi == most_hi && (uint32_t)u == most_lo && u != 0 ? (unsigned)i : (unsigned)kMaxE);
+}
+
+// eight experts of a lane, 32 apart
+template <typename T>
+__device__ __forceinline__ void read_eight(const RouteArgs& a, int64_t row, int e0, float (&x)[8])
+{
+    const T* p = static_cast<const T*>(a.logits) + row * a.ld;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = e0 + 32 * u < a.E ? to_f32(p[e0 + 32 * u]) : -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = seen(x[u], Type<T>::big);
+}
+__device__ __forceinline__ void read_eight(const RouteArgs& a, int64_t row, int e0, float (&x)[8])
+{
+    if (a.dtype == TAOT_F32) read_eight<float>(a, row, e0, x);
+    else if (a.dtype == TAOT_BF16) read_eight<__nv_bfloat16>(a, row, e0, x);
+    else read_eight<__half>(a, row, e0, x);
+}
+
+// a lane's largest key and the first expert that has it
+__device__ __forceinline__ void own_largest(const uint64_t* key, int E, uint64_t& u, int& i)
+{
+    u = 0;
+    i = kMaxE;
+    for (int e0 = threadIdx.x & 31; e0 < E; e0 += 256) {
+        uint64_t v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = e0 + 32 * q < E ? key[e0 + 32 * q] : 0ull;
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (v[q] > u) { u = v[q]; i = e0 + 32 * q; }
+    }
 }
 
 // The chosen experts of one row, by arithmetic in 64 bits, by a whole warp: lane j % 32 holds place j in at0 (j < 32) or at1, -1
 // where no expert is left.  key [E] is shared memory of the warp.  top and total: the largest open logit and the sum of
-// exp(logit - top).
-static __device__ __noinline__ void choose_exactly(const RouteArgs& a, int64_t row, double* key, int& at0, int& at1, float& top_out, float& total_out)
+// exp(logit - top).  Few rows come here, but a warp that has one is the last to end: loads and exponentials go eight at a time, and
+// a lane keeps its largest key at hand.
+static __device__ __noinline__ void choose_exactly(const RouteArgs& a, int64_t row, uint64_t* key, int& at0, int& at1, float& top_out, float& total_out)
 {
     const int lane = threadIdx.x & 31;
     const float* bias = a.bias ? a.bias + row / a.T * a.E : nullptr;
-    double top = -INFINITY, total = 0.0;
-    for (int e = lane; e < a.E; e += 32) {
-        const double x = logit_at(a.logits, row * a.ld + e, a.dtype);
-        key[e] = x;
-        top = fmax(top, x);
+    const bool scored = bias || a.groups > 1;                      // keys are scores
+    float top = -INFINITY;
+    for (int e0 = lane; e0 < a.E; e0 += 256) {
+        float x[8];
+        read_eight(a, row, e0, x);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            top = fmaxf(top, x[u]);
+            if (e0 + 32 * u < a.E) key[e0 + 32 * u] = ordered((double)x[u]);
+        }
     }
     top = warp_max(top);
+    double total = 0.0;
     if (a.score == TAOT_SOFTMAX && top > -INFINITY) {
-        for (int e = lane; e < a.E; e += 32) total += exp(key[e] - top);
+        for (int e0 = lane; e0 < a.E; e0 += 256) {
+            float x[8];
+            read_eight(a, row, e0, x);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) total += exp_of((double)x[u] - (double)top);
+        }
 #pragma unroll
         for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
     }
-    top_out = (float)top;
+    top_out = top;
     total_out = (float)total;
-    if (bias || a.groups > 1)
-        for (int e = lane; e < a.E; e += 32) {
-            const double x = key[e], b = bias ? (double)bias[e] : 0.0;
-            const double s = a.score == TAOT_SOFTMAX ? exp(x - top) / total : 1.0 / (1.0 + exp(-x));
-            key[e] = x > -INFINITY && isfinite(b) ? s + b : -INFINITY;
+    if (scored) {
+        const double inv = 1.0 / total;
+        for (int e0 = lane; e0 < a.E; e0 += 256) {
+            float x[8], b[8];
+            read_eight(a, row, e0, x);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) b[u] = bias && e0 + 32 * u < a.E ? bias[e0 + 32 * u] : 0.0f;
+            double s[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s[u] = exp_of(a.score == TAOT_SOFTMAX ? (double)x[u] - (double)top : -(double)x[u]);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                s[u] = a.score == TAOT_SOFTMAX ? s[u] * inv : __drcp_rn(1.0 + s[u]);
+                if (e0 + 32 * u < a.E) key[e0 + 32 * u] = x[u] > -INFINITY && isfinite(b[u]) ? ordered(s[u] + (double)b[u]) : 0ull;
+            }
         }
+    }
     __syncwarp();
     if (a.groups > 1) {
         const int size = a.E / a.groups;
-        double score0 = -INFINITY, score1 = -INFINITY;             // of groups lane and lane + 32
+        uint64_t score0 = 0, score1 = 0;                           // of groups lane and lane + 32
         for (int g = lane; g < a.groups; g += 32) {
-            double m1 = -INFINITY, m2 = -INFINITY;
-            for (int e = g * size; e < (g + 1) * size; ++e) {
-                const double v = key[e];
-                m2 = fmax(m2, fmin(m1, v));
-                m1 = fmax(m1, v);
+            uint64_t m1 = 0, m2 = 0;
+            int e = lane % size;                                   // (each lane from another place on: other banks)
+#pragma unroll 8
+            for (int i = 0; i < size; ++i) {
+                const uint64_t v = key[g * size + e];
+                e = e + 1 == size ? 0 : e + 1;
+                m2 = max(m2, min(m1, v));
+                m1 = max(m1, v);
             }
-            const double s = a.top == 2 && m2 > -INFINITY ? m1 + m2 : m1;
+            const uint64_t s = a.top == 2 && m2 ? ordered(number_of(m1) + number_of(m2)) : m1;
             if (g < 32) score0 = s; else score1 = s;
         }
         uint64_t kept = 0, left = a.groups == 64 ? ~0ull : (1ull << a.groups) - 1;
         for (int i = 0; i < a.kept; ++i) {
-            const bool l0 = left >> lane & 1, l1 = left >> (lane + 32) & 1;
-            const double v0 = l0 ? score0 : -INFINITY, v1 = l1 ? score1 : -INFINITY;
-            int g = v1 > v0 ? warp_argmax(v1, lane + 32) : warp_argmax(v0, lane);
+            const uint64_t v0 = left >> lane & 1 ? score0 : 0ull, v1 = left >> (lane + 32) & 1 ? score1 : 0ull;
+            const bool second = v1 > v0;
+            int g = warp_argmax(second ? v1 : v0, second ? lane + 32 : lane);
             if (g == kMaxE) g = __ffsll((long long)left) - 1;      // groups without open experts come last, in order
             kept |= 1ull << g;
             left &= ~(1ull << g);
         }
-        for (int e = lane; e < a.E; e += 32) {
-            const bool in_group = (kept >> (e / size)) & 1;
-            if (!in_group) key[e] = -INFINITY;
-            else if (!bias) key[e] = logit_at(a.logits, row * a.ld + e, a.dtype);
+        for (int e0 = lane; e0 < a.E; e0 += 256) {
+            float x[8];
+            if (!bias) read_eight(a, row, e0, x);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int e = e0 + 32 * u;
+                if (e >= a.E) continue;
+                if (!((kept >> (e / size)) & 1)) key[e] = 0ull;
+                else if (!bias) key[e] = ordered((double)x[u]);
+            }
         }
     }
-    // a lane's own largest, renewed by the lane that loses it
-    double v = -INFINITY;
-    int i = kMaxE;
-    for (int e = lane; e < a.E; e += 32)
-        if (key[e] > v) { v = key[e]; i = e; }
+    uint64_t v;
+    int i;
+    own_largest(key, a.E, v, i);
     at0 = at1 = -1;
     for (int j = 0; j < a.k; ++j) {
         const int e = warp_argmax(v, i);
@@ -140,11 +235,8 @@ static __device__ __noinline__ void choose_exactly(const RouteArgs& a, int64_t r
             if (j < 32) at0 = e; else at1 = e;
         }
         if (e == i) {
-            key[e] = -INFINITY;
-            v = -INFINITY;
-            i = kMaxE;
-            for (int f = lane; f < a.E; f += 32)
-                if (key[f] > v) { v = key[f]; i = f; }
+            key[e] = 0ull;
+            own_largest(key, a.E, v, i);
         }
     }
     __syncwarp();
@@ -291,6 +383,114 @@ __device__ __forceinline__ float score_of(int32_t score, const Scores& s, float 
 __device__ __forceinline__ float score_error(int32_t score, const Scores& s, int terms)
 {
     return score == TAOT_SIGMOID ? 4e-7f : s.inv * ((float)(terms + 16) * 1.2e-7f);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// What fp32 leaves open, settled in 64 bits for the few experts that it is open for.  A warp works on one row.  Few rows come here,
+// but a warp that has one is the last to end, and its code is not in the instruction cache: it is kept short.
+
+// the key of a chosen form in 64 bits: the score (+ bias), or the logit
+__device__ __forceinline__ uint64_t exact_key(const RouteArgs& a, const float* bias, bool scored, int64_t row, int e, float top, double inv)
+{
+    const float x = logit_at(a.logits, row * a.ld + e, a.dtype);
+    if (!scored) return ordered((double)x);
+    const float b = bias ? bias[e] : 0.0f;
+    double s = exp_of(a.score == TAOT_SOFTMAX ? (double)x - (double)top : -(double)x);
+    s = a.score == TAOT_SOFTMAX ? s * inv : __drcp_rn(1.0 + s);
+    return x > -INFINITY && isfinite(b) ? ordered(s + (double)b) : 0ull;
+}
+
+// the reciprocal of the sum of exp(logit - top) over a row
+__device__ __forceinline__ double exact_inverse(const RouteArgs& a, int64_t row, float top)
+{
+    double total = 0.0;
+    for (int e = threadIdx.x & 31; e < a.E; e += 32) total += exp_of((double)logit_at(a.logits, row * a.ld + e, a.dtype) - (double)top);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
+    return 1.0 / total;
+}
+
+// The experts of a row that may matter: those of the groups in `kept` whose key in fp32 is at least `least` of their group (held by
+// lane at + group * step).  Up to 32 of them go to `found`; returns how many there are.
+__device__ __forceinline__ int gather(const RouteArgs& a, const float* bias, bool scored, int64_t row, const Scores& sc, uint32_t kept, float least,
+                                      int at, int step, int32_t* found)
+{
+    const int lane = threadIdx.x & 31, size = a.E / a.groups;
+    int count = 0;
+#pragma unroll 2
+    for (int e0 = 0; e0 < a.E; e0 += 32) {
+        const int e = e0 + lane, g = min(e, a.E - 1) / size;
+        float v = e < a.E ? logit_at(a.logits, row * a.ld + e, a.dtype) : -INFINITY;
+        if (scored && bias && v > -INFINITY) {
+            const float b = bias[e];
+            v = isfinite(b) ? score_of(a.score, sc, v) + b : -INFINITY;
+        }
+        const float limit = __shfl_sync(kAll, least, at + g * step);
+        const bool hit = v > -INFINITY && v >= limit && (kept >> g & 1);
+        const unsigned all = __ballot_sync(kAll, hit);
+        const int place = count + __popc(all & ((1u << lane) - 1));
+        if (hit && place < 32) found[place] = e;
+        count += __popc(all);
+    }
+    __syncwarp();
+    return count;
+}
+
+// Which groups are kept (of at most 8), where their scores in fp32 are too close: from the experts whose keys are at least `least`, a
+// lower bound of the last key that counts in a group.  Returns false where there are too many of them.
+static __device__ __noinline__ bool settle_groups(const RouteArgs& a, int64_t row, const Scores sc, float least, int at, int step, int32_t* found, uint32_t& kept)
+{
+    const int lane = threadIdx.x & 31, size = a.E / a.groups;
+    const float* bias = a.bias ? a.bias + row / a.T * a.E : nullptr;
+    const int count = gather(a, bias, true, row, sc, 0xffffffffu, least, at, step, found);
+    if (count > 32) return false;
+    const double inv = a.score == TAOT_SOFTMAX ? exact_inverse(a, row, sc.top) : 1.0;
+    const int e = lane < count ? found[lane] : 0;
+    const uint64_t mine = lane < count ? exact_key(a, bias, true, row, e, sc.top, inv) : 0ull;
+    uint64_t score = 0;                                            // of group `lane`
+    for (int g = 0; g < a.groups; ++g) {
+        uint64_t u = lane < count && e / size == g ? mine : 0ull, m[2] = {0, 0};
+        for (int i = 0; i < a.top; ++i) {
+            const int who = warp_argmax(u, lane);
+            if (who == kMaxE) break;
+            m[i] = __shfl_sync(kAll, u, who);
+            if (lane == who) u = 0;
+        }
+        if (lane == g) score = m[1] ? ordered(number_of(m[0]) + number_of(m[1])) : m[0];
+    }
+    int rank = 0;
+    for (int g = 0; g < a.groups; ++g) {
+        const uint64_t u = __shfl_sync(kAll, score, g);
+        if (u > score || (u == score && g < lane)) ++rank;
+    }
+    kept = __ballot_sync(kAll, lane < a.groups && rank < a.kept);
+    __syncwarp();
+    return true;
+}
+
+// The chosen experts of a row (at most 16, lane j has place j) from those whose key in fp32 is at least `least`, a lower bound of
+// the last chosen one's.  Returns false where there are too many of them.
+static __device__ __noinline__ bool settle_choice(const RouteArgs& a, int64_t row, const Scores sc, uint32_t kept, float least, int32_t* found, int& place)
+{
+    const int lane = threadIdx.x & 31;
+    const float* bias = a.bias ? a.bias + row / a.T * a.E : nullptr;
+    const int count = gather(a, bias, bias != nullptr, row, sc, kept, least, 0, 0, found);
+    if (count > 32) return false;
+    const double inv = bias && a.score == TAOT_SOFTMAX ? exact_inverse(a, row, sc.top) : 1.0;
+    const int e = lane < count ? found[lane] : kMaxE;
+    const uint64_t mine = lane < count ? exact_key(a, bias, bias != nullptr, row, e, sc.top, inv) : 0ull;
+    int rank = 0;
+    for (int i = 0; i < count; ++i) {
+        const uint64_t u = __shfl_sync(kAll, mine, i);
+        const int f = __shfl_sync(kAll, e, i);
+        if (u > mine || (u == mine && f < e)) ++rank;
+    }
+    __syncwarp();
+    if (lane < count) found[rank] = e;
+    __syncwarp();
+    place = lane < min(a.k, count) ? found[lane] : -1;
+    __syncwarp();
+    return true;
 }
 
 // four consecutive logits as numbers

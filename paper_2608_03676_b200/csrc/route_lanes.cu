@@ -54,7 +54,7 @@ template <typename T, int K, int U, bool BIAS, bool GROUP, bool WIDE>
 __global__ void __launch_bounds__(kWarps * 32)
 route_lanes_kernel(const __grid_constant__ RouteArgs a)
 {
-    extern __shared__ double keys[];
+    extern __shared__ uint64_t keys[];
     constexpr int kOwn = K / kLanes;                               // places of the list that a lane stands for
     constexpr uint32_t kSlots = 4 * K - 1;
     constexpr bool kExact = !BIAS && sizeof(T) == 2;               // keys lose nothing
@@ -103,20 +103,28 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
         uint32_t list[K];
 #pragma unroll
         for (int u = 0; u < K; ++u) list[u] = 0;
+        float xs[U][4], bs[BIAS ? U : 1][4];                       // (read before any of them is used)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u;
+            const int c = min(GROUP ? sub * per + i : i * kLanes + sub, C - 1);
+            load_chunk<T, WIDE>(x_row, c, a.E, xs[u]);
+            if (BIAS) {
+                if (WIDE) four(b_row + 4 * c, bs[u]);
+                else
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) bs[u][q] = 4 * c + q < a.E ? b_row[4 * c + q] : INFINITY;
+            }
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u;
             const int c = GROUP ? sub * per + i : i * kLanes + sub;
             if (i >= per || c >= C) continue;
-            float x[4], m = -INFINITY;
-            load_chunk<T, WIDE>(x_row, c, a.E, x);
+            float (&x)[4] = xs[u];
+            float m;
             if (BIAS) {
-                float b[4];
-                if (WIDE) four(b_row + 4 * c, b);
-                else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) b[q] = 4 * c + q < a.E ? b_row[4 * c + q] : INFINITY;
-                }
+                const float (&b)[4] = bs[u];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     x[q] = x[q] > -big && fabsf(b[q]) < INFINITY ? score_of(a.score, sc, fminf(x[q], big)) + b[q] : -INFINITY;
@@ -144,7 +152,10 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             merge_list<!kExact>(best, list, lost);
         }
     }
+    uint64_t* const scratch = keys + (threadIdx.x >> 5) * max(a.E, 16);
+    int32_t* const found = reinterpret_cast<int32_t*>(scratch);
     bool redo = false;
+    uint32_t kept_groups = 1u;
     if (GROUP) {
         const int lanes = kLanes / a.groups;                       // of a group
         for (int o = 1; o < lanes; o *= 2) {
@@ -166,10 +177,26 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             const int h = (sub ^ o) / lanes;
             if (h != g && (sub ^ o) % lanes == 0 && (other > score || (other == score && h < g))) ++rank;
         }
-        const bool kept = rank < a.kept;
+        bool kept = rank < a.kept;
         const float worst = row_min(kept ? score : INFINITY), next = row_max(kept ? -INFINITY : score);
         const float size = row_max(s1 > -INFINITY ? fmaxf(fabsf(s1), s2 > -INFINITY ? fabsf(s2) : 0.0f) : 0.0f);
-        redo = a.kept < a.groups && !(worst - next > 4.0f * off + 8.0f * size * 1.2e-7f);
+        const bool close = routed && a.kept < a.groups && !(worst - next > 4.0f * off + 8.0f * size * 1.2e-7f);
+        // (a key that counts in a group is at most twice the error below the last one that counts here)
+        const float least = (a.top == 2 ? g2 : g1) - (BIAS ? 2.0f * off + 2.4e-7f * size : 0.0f);
+        for (unsigned left = __ballot_sync(kAll, close); left;) {
+            const int from = (__ffs(left) - 1) & ~(kLanes - 1);
+            left &= ~(((1u << kLanes) - 1) << from);
+            const Scores s = {__shfl_sync(kAll, sc.top, from), __shfl_sync(kAll, sc.inv, from)};
+            uint32_t groups;
+            const bool settled = settle_groups(a, first + from / kLanes, s, least, from, lanes, found, groups);
+            if ((lane & ~(kLanes - 1)) == from) {
+                if (settled) kept = groups >> g & 1;
+                else redo = true;
+            }
+        }
+        kept_groups = 0;
+        const unsigned votes = __ballot_sync(kAll, kept) >> (lane & ~(kLanes - 1));
+        for (int h = 0; h < a.groups; ++h) kept_groups |= (votes >> (h * lanes) & 1) << h;
         if (!kept) {
 #pragma unroll
             for (int i = 0; i < K; ++i) best[i] = 0;
@@ -241,6 +268,8 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
         x[h] = there ? seen(to_f32(x_row[at[h]]), big) : -INFINITY;
         v[h] = x[h];
     }
+    bool settle = false;
+    float least = -INFINITY;                                       // a lower bound of the last chosen one's key
     if (!kExact) {
         // Is what was left out far enough below the last chosen one (the k-th, or the last there is)?  And are neighbours in order?
         uint32_t beyond = lost, last = 0;
@@ -298,9 +327,11 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
                 if (wraps && h == kOwn - 1) e = -1;
                 if (e >= 0 && !(v[h] - u > err) && !(x[h] == y && b[h] == c && at[h] < e)) fine = false;
             }
-            const float least = row_min(fminf(v[0] > -INFINITY ? v[0] : INFINITY, v[kOwn - 1] > -INFINITY ? v[kOwn - 1] : INFINITY));
+            least = row_min(fminf(v[0] > -INFINITY ? v[0] : INFINITY, v[kOwn - 1] > -INFINITY ? v[kOwn - 1] : INFINITY));
             if (beyond != 0 && !(least > number_of(beyond | drop) + err)) fine = false;
+            least -= err;
         } else if (!lossless) {
+            least = last ? number_of(last & ~drop) : -INFINITY;
             if (beyond != 0 && ((beyond ^ last) & ~drop) == 0) fine = false;
             if (K == 8) {
                 const float after = __shfl_down_sync(kAll, x[0], 1);
@@ -312,7 +343,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             }
         }
         const unsigned bad = __ballot_sync(kAll, !fine);
-        redo = redo || ((bad >> (lane & ~(kLanes - 1))) & ((1u << kLanes) - 1)) != 0;
+        settle = routed && !redo && ((bad >> (lane & ~(kLanes - 1))) & ((1u << kLanes) - 1)) != 0;
     }
     redo = redo && routed;
     if (!routed) {
@@ -339,19 +370,22 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
     }
 #pragma unroll
     for (int h = 0; h < kOwn; ++h)
-        if (mine < a.N && !redo && sub + kLanes * h < a.k) {
+        if (mine < a.N && !redo && !settle && sub + kLanes * h < a.k) {
             a.topk[row * a.k + sub + kLanes * h] = at[h];
             if (a.weights) a.weights[row * a.k + sub + kLanes * h] = a.scale * w[h];
         }
     if (BIAS || GROUP || !kExact) {
-        unsigned again = __ballot_sync(kAll, redo);
-        while (again) {
-            const int from = __ffs(again) - 1;
-            again &= ~(((1u << kLanes) - 1) << (from & ~(kLanes - 1)));
+        for (unsigned left = __ballot_sync(kAll, settle || redo); left;) {
+            const int from = (__ffs(left) - 1) & ~(kLanes - 1);
+            left &= ~(((1u << kLanes) - 1) << from);
             const int64_t r = first + from / kLanes;
-            int at0, at1;
-            float t, z;
-            choose_exactly(a, r, keys + (threadIdx.x >> 5) * a.E, at0, at1, t, z);
+            const Scores s = {__shfl_sync(kAll, sc.top, from), __shfl_sync(kAll, sc.inv, from)};
+            const float limit = __shfl_sync(kAll, least, from);
+            const uint32_t groups = __shfl_sync(kAll, kept_groups, from);
+            int at0 = -1, at1 = -1;
+            float t = s.top, z = __shfl_sync(kAll, total, from);
+            if (__shfl_sync(kAll, (int)redo, from) || !settle_choice(a, r, s, groups, limit, found, at0))
+                choose_exactly(a, r, scratch, at0, at1, t, z);
             write_row(a, r, at0, at1, t, z);
         }
     }
@@ -361,7 +395,7 @@ template <typename T, int K, int U, bool WIDE>
 cudaError_t launch(const RouteArgs& a, cudaStream_t st)
 {
     const unsigned grid = (unsigned)((a.N + kWarps * kRows - 1) / (kWarps * kRows));
-    const size_t scratch = sizeof(double) * kWarps * a.E;
+    const size_t scratch = sizeof(uint64_t) * kWarps * (a.E > 16 ? a.E : 16);
     if (a.groups > 1) {
         if (a.bias) route_lanes_kernel<T, K, U, true, true, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
         else route_lanes_kernel<T, K, U, false, true, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
