@@ -102,6 +102,41 @@ __device__ __forceinline__ void write8(T* row, int c, int D, bool wide, const Ru
     }
 }
 
+// A warp's 256 columns from c0 on, eight per lane.  WIDE (rows of whole runs that are read 16 bytes at a time): consecutive ones;
+// otherwise 32 apart, so that the lanes of a load are next to each other.  What is beyond D is read from the last columns
+// instead, without a branch, and not written.
+template <bool WIDE, typename T>
+__device__ __forceinline__ Run8<T> load8(const T* row, int c0, int lane, int D)
+{
+    Run8<T> r;
+    if constexpr (WIDE) {
+        const uint4* p = reinterpret_cast<const uint4*>(row + min(c0 + 8 * lane, D - 8));
+        uint4* q = reinterpret_cast<uint4*>(&r);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(Run8<T>) / 16; ++i) q[i] = p[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = row[min(c0 + 32 * i + lane, D - 1)];
+    }
+    return r;
+}
+template <bool WIDE, typename T>
+__device__ __forceinline__ void store8(T* row, int c0, int lane, int D, const Run8<T>& r)
+{
+    if constexpr (WIDE) {
+        const int c = c0 + 8 * lane;
+        uint4* p = reinterpret_cast<uint4*>(row + c);
+        const uint4* q = reinterpret_cast<const uint4*>(&r);
+        if (c < D)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(Run8<T>) / 16; ++i) p[i] = q[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c0 + 32 * i + lane < D) row[c0 + 32 * i + lane] = r.v[i];
+    }
+}
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
