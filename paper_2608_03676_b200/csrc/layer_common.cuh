@@ -102,38 +102,47 @@ __device__ __forceinline__ void write8(T* row, int c, int D, bool wide, const Ru
     }
 }
 
-// A warp's 256 columns from c0 on, eight per lane.  WIDE (rows of whole runs that are read 16 bytes at a time): consecutive ones;
-// otherwise 32 apart, so that the lanes of a load are next to each other.  What is beyond D is read from the last columns
-// instead, without a branch, and not written.
+// A warp's 256 columns from c0 on, eight per lane: WIDE (rows of a multiple of eight columns that can be read 16 bytes at a time) in
+// pieces of 16 bytes, those of a load next to each other; otherwise one by one, 32 apart.  The column of a lane's element i:
+template <bool WIDE, typename T>
+__device__ __forceinline__ int column(int c0, int lane, int i)
+{
+    if (!WIDE) return c0 + 32 * i + lane;
+    return sizeof(T) == 2 ? c0 + 8 * lane + i : c0 + 128 * (i >> 2) + 4 * lane + (i & 3);
+}
+// What is beyond D is read from the last columns instead, without a branch, and not written.
 template <bool WIDE, typename T>
 __device__ __forceinline__ Run8<T> load8(const T* row, int c0, int lane, int D)
 {
+    constexpr int kPiece = 16 / (int)sizeof(T);
     Run8<T> r;
     if constexpr (WIDE) {
-        const uint4* p = reinterpret_cast<const uint4*>(row + min(c0 + 8 * lane, D - 8));
         uint4* q = reinterpret_cast<uint4*>(&r);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(Run8<T>) / 16; ++i) q[i] = p[i];
+        for (int i = 0; i < 8; i += kPiece) q[i / kPiece] = *reinterpret_cast<const uint4*>(row + min(column<WIDE, T>(c0, lane, i), D - kPiece));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = row[min(c0 + 32 * i + lane, D - 1)];
+        for (int i = 0; i < 8; ++i) r.v[i] = row[min(column<WIDE, T>(c0, lane, i), D - 1)];
     }
     return r;
 }
 template <bool WIDE, typename T>
 __device__ __forceinline__ void store8(T* row, int c0, int lane, int D, const Run8<T>& r)
 {
+    constexpr int kPiece = 16 / (int)sizeof(T);
     if constexpr (WIDE) {
-        const int c = c0 + 8 * lane;
-        uint4* p = reinterpret_cast<uint4*>(row + c);
         const uint4* q = reinterpret_cast<const uint4*>(&r);
-        if (c < D)
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(Run8<T>) / 16; ++i) p[i] = q[i];
+        for (int i = 0; i < 8; i += kPiece) {
+            const int c = column<WIDE, T>(c0, lane, i);
+            if (c < D) *reinterpret_cast<uint4*>(row + c) = q[i / kPiece];
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c0 + 32 * i + lane < D) row[c0 + 32 * i + lane] = r.v[i];
+        for (int i = 0; i < 8; ++i) {
+            const int c = column<WIDE, T>(c0, lane, i);
+            if (c < D) row[c] = r.v[i];
+        }
     }
 }
 

@@ -19,6 +19,7 @@ struct NormArgs {
     uint8_t* q;
     float *scales, *rstd;
     int64_t ld_x, ld_residual, ld_h, ld_y, ld_q;
+    int64_t N;
     int32_t D, group, scale_cols, wide;
     float eps;
 };
@@ -99,6 +100,131 @@ rms_norm_kernel(NormArgs a)
     }
 }
 
+// the sum of n warps' values (n a power of two up to 16), by each warp
+template <int n>
+__device__ __forceinline__ float sum_of_warps(const float* part)
+{
+    float v = part[threadIdx.x & (n - 1)];
+#pragma unroll
+    for (int o = n / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// Rows of up to 8192 columns: `kLanes` threads hold a row, `kRuns` runs of eight columns each, from the addition to the 8-bit form.
+template <typename T, int kLanes, int kRuns, bool WIDE>
+__global__ void __launch_bounds__(kLanes > kThreads ? kLanes : kThreads, WIDE && sizeof(T) == 2 && kLanes <= kThreads ? (kRuns == 1 ? 6 : 5) : 1)
+rms_norm_row_kernel(const __grid_constant__ NormArgs a)
+{
+    constexpr int kCta = kLanes > kThreads ? kLanes : kThreads;
+    constexpr int kWarpsOfRow = kLanes / 32;
+    __shared__ float part[kCta / 32];
+    const int tid = threadIdx.x, lane = tid & 31, slot = tid / kLanes, start = (tid % kLanes >> 5) * 256;
+    const int64_t row = (int64_t)blockIdx.x * (kCta / kLanes) + slot;
+    const bool there = row < a.N;
+    const auto live = [&](int r, int i) { return there && column<WIDE, T>(start + r * kLanes * 8, lane, i) < a.D; };
+    Run8<T> h[kRuns], w[kRuns];
+    float sum = 0.0f;
+    if (there) {
+        const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) h[r] = load8<WIDE>(x, start + r * kLanes * 8, lane, a.D);
+        if (a.residual) {
+            const T* res = static_cast<const T*>(a.residual) + row * a.ld_residual;
+            Run8<T> e[kRuns];
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r) e[r] = load8<WIDE>(res, start + r * kLanes * 8, lane, a.D);
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r) {
+                float f[8], g[8];
+                widen(h[r], f);
+                widen(e[r], g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] += g[i];
+                h[r] = narrowed<T>(f);
+                store8<WIDE>(static_cast<T*>(a.h) + row * a.ld_h, start + r * kLanes * 8, lane, a.D, h[r]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+            w[r] = load8<WIDE>(static_cast<const T*>(a.weight), start + r * kLanes * 8, lane, a.D);
+            float f[8];
+            widen(h[r], f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (live(r, i)) sum = fmaf(f[i], f[i], sum);
+        }
+    }
+    // (divided by D before the sums of the threads are added: those squares may add up to more than the mean may be)
+    sum = warp_sum(sum * (1.0f / (float)a.D));
+    if (kWarpsOfRow > 1) {
+        if (lane == 0) part[tid >> 5] = sum;
+        __syncthreads();
+        sum = sum_of_warps<kWarpsOfRow>(part + slot * kWarpsOfRow);
+    }
+    if (!there) return;                            // (whole warps)
+    const float rstd = 1.0f / sqrtf(sum + a.eps);
+    if (a.rstd && tid % kLanes == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r) {
+        const int c0 = start + r * kLanes * 8;
+        float f[8], g[8];
+        widen(h[r], f);
+        widen(w[r], g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = live(r, i) ? f[i] * rstd * g[i] : 0.0f;
+        if (a.y) store8<WIDE>(static_cast<T*>(a.y) + row * a.ld_y, c0, lane, a.D, narrowed<T>(f));
+        if (!a.q || c0 >= a.D) continue;           // (the same for a warp)
+        if (WIDE && sizeof(T) == 2) {
+            write_eight_bit(a, row, c0 + 8 * lane, f);
+        } else if (WIDE) {
+            // columns 4 lane to 4 lane + 3 of either half of the warp's 256
+            float most[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) most[q] = max_nan(max_nan(fabsf(f[4 * q]), fabsf(f[4 * q + 1])), max_nan(fabsf(f[4 * q + 2]), fabsf(f[4 * q + 3])));
+            if (a.group == 256) most[0] = most[1] = max_nan(most[0], most[1]);
+            for (int o = 1; o < min(a.group >> 2, 32); o <<= 1) {
+                most[0] = max_nan(most[0], __shfl_xor_sync(0xffffffffu, most[0], o));
+                most[1] = max_nan(most[1], __shfl_xor_sync(0xffffffffu, most[1], o));
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int c = column<WIDE, T>(c0, lane, 4 * q);
+                const float scale = max_nan(most[q] / kE4m3Max, kLeastScale), by = 1.0f / scale;
+                if (c >= a.D) continue;
+                if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + c / a.group] = scale;
+                uint32_t word = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) word |= (uint32_t)__nv_cvt_float_to_fp8(f[4 * q + i] * by, __NV_SATFINITE, __NV_E4M3) << (8 * i);
+                *reinterpret_cast<uint32_t*>(a.q + row * a.ld_q + c) = word;
+            }
+        } else {
+            // column 32 i + lane of the warp's 256: a group is 1, 2, 4 or 8 of the i
+            float most[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most[i] = fabsf(f[i]);
+            const int n = a.group >> 5;
+#pragma unroll
+            for (int o = 1; o < 8; o *= 2)
+                if (o < n) {
+                    float other[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) other[i] = most[i ^ o];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most[i] = max_nan(most[i], other[i]);
+                }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int o = 16; o; o >>= 1) most[i] = max_nan(most[i], __shfl_xor_sync(0xffffffffu, most[i], o));
+                const float scale = max_nan(most[i] / kE4m3Max, kLeastScale);
+                const int c = c0 + 32 * i + lane;
+                if (lane == 0 && (i & (n - 1)) == 0 && c < a.D) a.scales[row * a.scale_cols + c / a.group] = scale;
+                if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(f[i] * (1.0f / scale), __NV_SATFINITE, __NV_E4M3);
+            }
+        }
+    }
+}
+
 struct NormGradArgs {
     const void *dy, *dh, *h, *weight;
     const float* rstd;
@@ -174,7 +300,209 @@ rms_norm_dw_sum_kernel(NormGradArgs a)
     a.dweight[c] = sum;
 }
 
-constexpr int kParts = 128;
+// dx and the sums for dweight in one pass over the rows: `kLanes` threads hold a row, `kRuns` runs of eight columns each, and keep the
+// weights and the sums of their columns in registers for all rows that they take, one after another.  The rows to come are
+// on their way to shared memory meanwhile, kStages of them (each thread copies, waits for and reads its own columns: no
+// barrier is needed for that); rows that cannot be copied 16 bytes at a time are read when they are due.  A CTA's sums go to the
+// workspace (rms_norm_dw_join_kernel).
+constexpr int kParts = 592;                        // CTAs, four for each of the 148 SMs
+
+template <typename T, int kLanes, int kRuns>
+struct GradShape {
+    static constexpr int kCta = kLanes > kThreads ? kLanes : kThreads;
+    static constexpr int kRows = kCta / kLanes;    // at a time
+    static constexpr int kPieces = kRuns * (int)sizeof(Run8<T>) / 16;        // 16-byte pieces of a thread, row and array
+    // 1024 runs per SM, whose rows to come take 196 KB: four of 16 bits, two of fp32
+    static constexpr int kStages = sizeof(T) == 2 ? (kRuns == 4 ? 2 : 4) : 2;
+    static constexpr int kCtasPerSm = kRuns == 4 ? 1 : 1024 / (kCta * kRuns);
+    static constexpr size_t kRing = (size_t)kStages * 3 * kPieces * 16 * kCta;
+    static constexpr size_t kSums = sizeof(float) * kCta * 8 * kRuns;
+};
+
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async_word(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_queued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int n>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory"); }
+
+template <typename T, int kLanes, int kRuns, bool WIDE>
+__global__ void __launch_bounds__(GradShape<T, kLanes, kRuns>::kCta, WIDE ? GradShape<T, kLanes, kRuns>::kCtasPerSm : kLanes > kThreads ? 1 : 2)
+rms_norm_grad_kernel(const __grid_constant__ NormGradArgs a)
+{
+    typedef GradShape<T, kLanes, kRuns> S;
+    constexpr bool kAsync = WIDE || sizeof(T) == 4;
+    constexpr int kStages = kAsync ? S::kStages : 1;
+    constexpr int kWarpsOfRow = kLanes / 32;
+    extern __shared__ __align__(16) uint4 ring[];  // [stage][array][piece][thread]
+    __shared__ float part[2][S::kCta / 32];
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int slot = tid / kLanes, start = (tid % kLanes >> 5) * 256;       // first column of the warp's runs, which are kLanes * 8 apart
+    const auto live = [&](int r, int i) { return column<WIDE, T>(start + r * kLanes * 8, lane, i) < a.D; };
+    taot_release();                                // (the next kernel's CTAs come as these end)
+    Run8<T> w[kRuns];
+    float dw[kRuns][8];
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r) {
+        w[r] = load8<WIDE>(static_cast<const T*>(a.weight), start + r * kLanes * 8, lane, a.D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[r][i] = 0.0f;
+    }
+    const auto array = [&](int which, int64_t row) {
+        return which == 0 ? static_cast<const T*>(a.dy) + row * a.ld_dy : which == 1 ? static_cast<const T*>(a.h) + row * a.ld_h : static_cast<const T*>(a.dh) + row * a.ld_dh;
+    };
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + (WIDE ? 16u : 4u) * (uint32_t)tid;
+    float rstd[kStages];
+    const auto queue = [&](int stage, int64_t row) {               // (an empty group where there is no such row)
+        if (row < a.N) {
+            rstd[stage] = a.rstd[row];
+#pragma unroll
+            for (int which = 0; which < 3; ++which) {
+                if (which == 2 && !a.dh) break;
+                const T* from = array(which, row);
+#pragma unroll
+                for (int r = 0; r < kRuns; ++r)
+                    if (!WIDE) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (live(r, i))
+                                copy_async_word(ring_at + 4u * (uint32_t)((((stage * 3 + which) * kRuns + r) * 8 + i) * S::kCta), from + column<WIDE, T>(start + r * kLanes * 8, lane, i));
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < S::kPieces / kRuns; ++q) {
+                            const int c = column<WIDE, T>(start + r * kLanes * 8, lane, q * (8 / (S::kPieces / kRuns)));
+                            if (c < a.D) copy_async(ring_at + 16u * (uint32_t)(((stage * 3 + which) * S::kPieces + r * (S::kPieces / kRuns) + q) * S::kCta), from + c);
+                        }
+                    }
+            }
+        }
+        copies_queued();
+    };
+    const auto take = [&](int stage, int which, int r, int64_t row) {
+        if constexpr (WIDE) {
+            Run8<T> v;
+            uint4* to = reinterpret_cast<uint4*>(&v);
+#pragma unroll
+            for (int q = 0; q < S::kPieces / kRuns; ++q) to[q] = ring[((stage * 3 + which) * S::kPieces + r * (S::kPieces / kRuns) + q) * S::kCta + tid];
+            return v;
+        } else if constexpr (kAsync) {
+            Run8<T> v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v.v[i] = reinterpret_cast<const T*>(ring)[(((stage * 3 + which) * kRuns + r) * 8 + i) * S::kCta + tid];
+            return v;
+        } else {
+            return load8<false>(array(which, row), start + r * kLanes * 8, lane, a.D);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * S::kRows;
+    int64_t first = (int64_t)blockIdx.x * S::kRows, row = first + slot;
+    const float inv = 1.0f / (float)a.D;
+    if (kAsync)
+#pragma unroll
+        for (int s = 0; s < kStages; ++s) queue(s, row + s * step);
+    int turn = 0;
+    while (first < a.N) {
+#pragma unroll
+        for (int s = 0; s < kStages; ++s) {
+            if (first >= a.N) break;                               // (the same for all threads of the CTA)
+            const bool there = row < a.N;
+            if (kAsync) copies_wait<kStages - 1>();
+            else if (there) rstd[0] = a.rstd[row];
+            float sum = 0.0f;
+            Run8<T> dy[kRuns], h[kRuns];
+            if (there)
+#pragma unroll
+                for (int r = 0; r < kRuns; ++r) {
+                    dy[r] = take(s, 0, r, row);
+                    h[r] = take(s, 1, r, row);
+                }
+            if (there)
+#pragma unroll
+                for (int r = 0; r < kRuns; ++r) {
+                    float d[8], x[8], f[8];
+                    widen(dy[r], d);
+                    widen(h[r], x);
+                    widen(w[r], f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (!live(r, i)) continue;
+                        const float t = x[i] * rstd[s];
+                        dw[r][i] = fmaf(d[i], t, dw[r][i]);
+                        sum = fmaf(d[i] * f[i], t, sum);
+                    }
+                }
+            sum = warp_sum(sum);
+            if (kWarpsOfRow > 1) {
+                if (lane == 0) part[turn][tid >> 5] = sum;
+                __syncthreads();
+                sum = sum_of_warps<kWarpsOfRow>(part[turn] + slot * kWarpsOfRow);
+            }
+            if (there) {
+                const float shift = rstd[s] * (sum * inv);
+#pragma unroll
+                for (int r = 0; r < kRuns; ++r) {
+                    float d[8], x[8], f[8];
+                    widen(dy[r], d);
+                    widen(h[r], x);
+                    widen(w[r], f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] = rstd[s] * (d[i] * f[i] - x[i] * shift);
+                    if (a.dh) {
+                        widen(take(s, 2, r, row), f);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) d[i] += f[i];
+                    }
+                    store8<WIDE>(static_cast<T*>(a.dx) + row * a.ld_dx, start + r * kLanes * 8, lane, a.D, narrowed<T>(d));
+                }
+            }
+            if (kAsync) queue(s, row + kStages * step);
+            turn ^= 1;
+            first += step;
+            row += step;
+        }
+    }
+    if (!a.dweight) return;
+    if (kAsync) copies_wait<0>();
+    __syncthreads();
+    // the rows that a CTA takes at a time have their own sums
+    float* const sums = reinterpret_cast<float*>(ring);
+    constexpr int kCols = kLanes * 8 * kRuns;
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[slot * kCols + column<WIDE, T>(start + r * kLanes * 8, lane, i)] = dw[r][i];
+    __syncthreads();
+    for (int c = tid; c < a.D; c += S::kCta) {
+        float s = 0.0f;
+#pragma unroll
+        for (int q = 0; q < S::kRows; ++q) s += sums[q * kCols + c];
+        a.part[(int64_t)blockIdx.x * a.D + c] = s;
+    }
+}
+
+// Adds up the CTAs' sums: a CTA takes 32 columns, a warp every 32nd of the CTAs.
+constexpr int kJoinThreads = 1024;
+__global__ void __launch_bounds__(kJoinThreads)
+rms_norm_dw_join_kernel(NormGradArgs a)
+{
+    __shared__ float part[kJoinThreads / 32][33];
+    taot_await();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (c < a.D)
+#pragma unroll 10
+        for (int p = warp; p < a.parts; p += kJoinThreads / 32) s += a.part[(int64_t)p * a.D + c];
+    part[warp][lane] = s;
+    __syncthreads();
+    s = warp_sum(part[lane][warp]);                // column `warp` of the CTA's
+    const int mine = blockIdx.x * 32 + warp;
+    if (lane == 0 && mine < a.D) a.dweight[mine] = s;
+}
 
 template <typename F>
 cudaError_t by_type(int32_t dtype, F&& f)
@@ -182,6 +510,68 @@ cudaError_t by_type(int32_t dtype, F&& f)
     if (dtype == TAOT_F32) return f(float());
     if (dtype == TAOT_BF16) return f(__nv_bfloat16());
     return f(__half());
+}
+
+template <typename T, bool WIDE, int kLanes, int kRuns>
+cudaError_t fused_as(NormGradArgs& a, cudaStream_t st)
+{
+    typedef GradShape<T, kLanes, kRuns> S;
+    const size_t ring = WIDE || sizeof(T) == 4 ? S::kRing : 0, sums = a.dweight ? S::kSums : 0, smem = ring > sums ? ring : sums;
+    const int64_t ctas = (a.N + S::kRows - 1) / S::kRows, most = kParts / 4 * (WIDE ? S::kCtasPerSm : S::kCta > kThreads ? 1 : 2);
+    a.parts = (int32_t)(ctas < most ? ctas : most);
+    const auto kernel = rms_norm_grad_kernel<T, kLanes, kRuns, WIDE>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<(unsigned)a.parts, S::kCta, smem, st>>>(a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess || !a.dweight) return e;
+    return taot_launch_chained(rms_norm_dw_join_kernel, (unsigned)((a.D + 31) / 32), (unsigned)kJoinThreads, 0, st, a);
+}
+
+// 16-bit rows: two runs of columns per thread (8192 rows of 4096: 56 us with one, 50 with two), fp32 rows and those that cannot be
+// copied 16 bytes at a time one; more where a CTA could not hold the row.
+template <typename T, bool WIDE>
+cudaError_t fused(NormGradArgs& a, cudaStream_t st)
+{
+    if (a.D <= 256) return fused_as<T, WIDE, 32, 1>(a, st);
+    if constexpr (sizeof(T) == 2 && WIDE) {
+        if (a.D <= 512) return fused_as<T, WIDE, 32, 2>(a, st);
+        if (a.D <= 1024) return fused_as<T, WIDE, 64, 2>(a, st);
+        if (a.D <= 2048) return fused_as<T, WIDE, 128, 2>(a, st);
+        if (a.D <= 4096) return fused_as<T, WIDE, 256, 2>(a, st);
+        if (a.D > 8192) return fused_as<T, WIDE, 512, 4>(a, st);
+    } else {
+        if (a.D <= 512) return fused_as<T, WIDE, 64, 1>(a, st);
+        if (a.D <= 1024) return fused_as<T, WIDE, 128, 1>(a, st);
+        if (a.D <= 2048) return fused_as<T, WIDE, 256, 1>(a, st);
+        if (a.D <= 4096) return fused_as<T, WIDE, 512, 1>(a, st);
+    }
+    return fused_as<T, WIDE, 512, 2>(a, st);
+}
+
+template <typename T, bool WIDE, int kLanes, int kRuns>
+cudaError_t by_row_as(const NormArgs& a, cudaStream_t st)
+{
+    constexpr int kCta = kLanes > kThreads ? kLanes : kThreads, kRows = kCta / kLanes;
+    rms_norm_row_kernel<T, kLanes, kRuns, WIDE><<<(unsigned)((a.N + kRows - 1) / kRows), kCta, 0, st>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, bool WIDE>
+cudaError_t by_row(const NormArgs& a, cudaStream_t st)
+{
+    if (a.D <= 256) return by_row_as<T, WIDE, 32, 1>(a, st);
+    if constexpr (WIDE) {
+        if (a.D <= 512) return by_row_as<T, WIDE, 32, 2>(a, st);
+        if (a.D <= 1024) return by_row_as<T, WIDE, 64, 2>(a, st);
+        if (a.D <= 2048) return by_row_as<T, WIDE, 128, 2>(a, st);
+        if (a.D <= 4096) return by_row_as<T, WIDE, 256, 2>(a, st);
+    } else {
+        if (a.D <= 512) return by_row_as<T, WIDE, 64, 1>(a, st);
+        if (a.D <= 1024) return by_row_as<T, WIDE, 128, 1>(a, st);
+        if (a.D <= 2048) return by_row_as<T, WIDE, 256, 1>(a, st);
+        if (a.D <= 4096) return by_row_as<T, WIDE, 512, 1>(a, st);
+    }
+    return by_row_as<T, WIDE, 512, 2>(a, st);
 }
 
 int check(const taot_norm_params* p)
@@ -224,9 +614,16 @@ extern "C" int taot_rms_norm(const taot_norm_params* p, const void* d_x, const v
     NormArgs a;
     a.x = d_x; a.residual = d_residual; a.weight = d_weight; a.h = d_h; a.y = d_y; a.q = d_q; a.scales = d_scales; a.rstd = d_rstd;
     a.ld_x = p->ld_x; a.ld_residual = p->ld_residual; a.ld_h = p->ld_h; a.ld_y = p->ld_y; a.ld_q = p->ld_q;
-    a.D = p->D; a.group = p->group; a.scale_cols = (int32_t)cols; a.eps = p->eps;
+    a.N = N; a.D = p->D; a.group = p->group; a.scale_cols = (int32_t)cols; a.eps = p->eps;
     a.wide = wide_rows(d_x, p->ld_x, e) && wide_rows(d_residual, p->ld_residual, e) && wide_rows(d_weight, 0, e) &&
              wide_rows(d_h, p->ld_h, e) && wide_rows(d_y, p->ld_y, e) && !misaligned(d_q, 8) && (!d_q || p->ld_q % 8 == 0);
+    if (D <= 8192) {                                       // beyond, two passes are faster (2048 x 16384 bf16: 72 us against 89)
+        a.wide = a.wide && D % 8 == 0;
+        TAOT_CUDA_OK(by_type(p->dtype, [&](auto t) {
+            return a.wide ? by_row<decltype(t), true>(a, static_cast<cudaStream_t>(stream)) : by_row<decltype(t), false>(a, static_cast<cudaStream_t>(stream));
+        }));
+        return TAOT_OK;
+    }
     TAOT_CUDA_OK(by_type(p->dtype, [&](auto t) {
         rms_norm_kernel<decltype(t)><<<(unsigned)N, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
         return cudaGetLastError();
@@ -276,9 +673,16 @@ extern "C" int taot_rms_norm_backward(const taot_norm_params* p, const void* d_d
     a.wide = wide_rows(d_dy, p->ld_y, e) && wide_rows(d_dh, p->ld_residual, e) && wide_rows(d_h, p->ld_h, e) &&
              wide_rows(d_weight, 0, e) && wide_rows(d_dx, p->ld_x, e);
     const unsigned cols = (unsigned)((D + kThreads - 1) / kThreads);
+    const bool wide = a.wide && D % 8 == 0;
+    if (D <= 8192 || (D <= 16384 && wide && e == 2)) {     // rows that the threads of a CTA can hold
+        a.wide = wide;
+        TAOT_CUDA_OK(by_type(p->dtype, [&](auto t) { return a.wide ? fused<decltype(t), true>(a, st) : fused<decltype(t), false>(a, st); }));
+        return TAOT_OK;
+    }
+    a.parts = 128;
     TAOT_CUDA_OK(by_type(p->dtype, [&](auto t) {
         if (d_dweight) {                                   // before dx, which may take the place of dy
-            rms_norm_dw_kernel<decltype(t)><<<dim3(cols, kParts), kThreads, 0, st>>>(a);
+            rms_norm_dw_kernel<decltype(t)><<<dim3(cols, (unsigned)a.parts), kThreads, 0, st>>>(a);
             rms_norm_dw_sum_kernel<<<cols, kThreads, 0, st>>>(a);
         }
         rms_norm_dx_kernel<decltype(t)><<<(unsigned)N, kThreads, 0, st>>>(a);

@@ -31,63 +31,143 @@ struct RouteGradArgs {
     int32_t E, k, score, renormalise, dtype;
 };
 
-__device__ __forceinline__ void put(void* p, int64_t i, int32_t dtype, float v)
+// kLanes lanes hold a row, kRuns runs of eight experts each: what reaches every expert (nothing, or for a softmax that is not
+// renormalised -c p_e sum_j g_j p_j) is written first, then the chosen experts' whole value over it, each by the lane of its
+// first place.  WIDE: rows of whole runs, 16 bytes at a time.
+template <typename T, int kLanes, int kRuns, bool WIDE>
+struct Row {
+    int sub;
+    __device__ __forceinline__ int expert(int r, int i) const
+    {
+        if (!WIDE) return (r * 8 + i) * kLanes + sub;
+        return sizeof(T) == 2 ? (r * kLanes + sub) * 8 + i : r * kLanes * 8 + (i >> 2) * kLanes * 4 + 4 * sub + (i & 3);
+    }
+    __device__ __forceinline__ void read(const T* row, int E, int r, float (&x)[8]) const
+    {
+        constexpr int kPiece = 16 / (int)sizeof(T);
+        Run8<T> v;
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < 8; i += kPiece)
+                reinterpret_cast<uint4*>(&v)[i / kPiece] = *reinterpret_cast<const uint4*>(row + min(expert(r, i), E - kPiece));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v.v[i] = row[min(expert(r, i), E - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = expert(r, i) < E ? seen(to_f32(v.v[i]), Type<T>::big) : -INFINITY;
+    }
+    __device__ __forceinline__ void write(T* row, int E, int r, const float (&x)[8]) const
+    {
+        constexpr int kPiece = 16 / (int)sizeof(T);
+        const Run8<T> v = narrowed<T>(x);
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < 8; i += kPiece)
+                if (expert(r, i) < E) *reinterpret_cast<uint4*>(row + expert(r, i)) = reinterpret_cast<const uint4*>(&v)[i / kPiece];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (expert(r, i) < E) row[expert(r, i)] = v.v[i];
+        }
+    }
+};
+// 2^v to 2^-22 of itself, down to the smallest values
+__device__ __forceinline__ float exp2_of(float v)
 {
-    if (dtype == TAOT_F32) static_cast<float*>(p)[i] = v;
-    else if (dtype == TAOT_BF16) static_cast<__nv_bfloat16*>(p)[i] = from_f32<__nv_bfloat16>(v);
-    else static_cast<__half*>(p)[i] = from_f32<__half>(v);
+    float r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
 
-// One warp per row, which is put together in shared memory: what reaches every expert, then the chosen ones' share in the
-// order of their places.
-__global__ void __launch_bounds__(kWarps * 32)
-route_grad_kernel(RouteGradArgs a)
+template <int kLanes>
+__device__ __forceinline__ float lanes_max(float v)
 {
-    extern __shared__ float rows[];
+#pragma unroll
+    for (int o = 1; o < kLanes; o *= 2) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
+    return v;
+}
+template <int kLanes>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+#pragma unroll
+    for (int o = 1; o < kLanes; o *= 2) v += __shfl_xor_sync(kAll, v, o);
+    return v;
+}
+
+template <typename T, int kLanes, int kRuns, bool WIDE, bool DENSE>
+__global__ void __launch_bounds__(kWarps * 32)
+route_grad_kernel(const __grid_constant__ RouteGradArgs a)
+{
+    constexpr float big = Type<T>::big;
     const int lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    if (row >= a.N) return;
-    float* out = rows + (threadIdx.x >> 5) * a.E;
+    const int64_t first = ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * (32 / kLanes);
+    if (first >= a.N) return;
+    const int64_t mine = first + lane / kLanes, row = mine < a.N ? mine : a.N - 1;       // (lanes past the end write nothing)
+    const Row<T, kLanes, kRuns, WIDE> cols = {lane & (kLanes - 1)};
+    const T* x_row = static_cast<const T*>(a.logits) + row * a.ld;
+    T* out = static_cast<T*>(a.dlogits) + row * a.ld_out;
     int at[2];
-    float g[2], x[2], d[2];
+    float g[2], x[2], d[2], base[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int j = lane + 32 * h;
+        const int j = cols.sub + kLanes * h;
         at[h] = j < a.k ? a.topk[row * a.k + j] : -1;
-        if ((unsigned)at[h] >= (unsigned)a.E) at[h] = -1;
-        g[h] = at[h] >= 0 ? a.scale * a.dweights[row * a.k + j] : 0.0f;
-        x[h] = at[h] >= 0 ? logit_at(a.logits, row * a.ld + at[h], a.dtype) : -INFINITY;
+        g[h] = j < a.k ? a.scale * a.dweights[row * a.k + j] : 0.0f;
     }
-    if (a.score == TAOT_SOFTMAX && !a.renormalise) {
-        float top = -INFINITY, total = 0.0f;
-        for (int e = lane; e < a.E; e += 32) {
-            out[e] = logit_at(a.logits, row * a.ld + e, a.dtype);
-            top = fmaxf(top, out[e]);
-        }
-        top = warp_max(top);
-        if (top == -INFINITY) top = 0.0f;          // no open expert: every score is zero
-        for (int e = lane; e < a.E; e += 32) {
-            out[e] = expf(out[e] - top);
-            total += out[e];
-        }
-        total = fmaxf(warp_sum(total), FLT_MIN);
-        __syncwarp();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) d[h] = at[h] >= 0 ? g[h] * (out[at[h]] / total) : 0.0f;
-        const float all = warp_sum(d[0] + d[1]) / total;
-        __syncwarp();
-        for (int e = lane; e < a.E; e += 32) out[e] *= -all;
+    for (int h = 0; h < 2; ++h) {
+        if ((unsigned)at[h] >= (unsigned)a.E) { at[h] = -1; g[h] = 0.0f; }
+        x[h] = at[h] >= 0 ? seen(to_f32(x_row[at[h]]), big) : -INFINITY;
+    }
+    if (DENSE) {
+        float e[kRuns][8], top = -INFINITY, total = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+            cols.read(x_row, a.E, r, e[r]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, e[r][i]);
+        }
+        top = lanes_max<kLanes>(top);
+        if (top == -INFINITY) top = 0.0f;          // no open expert: every score is zero
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                e[r][i] = exp2_of((e[r][i] - top) * kLog2e);
+                total += e[r][i];
+            }
+        const float inv = 1.0f / fmaxf(lanes_sum<kLanes>(total), FLT_MIN);
+        float p[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            p[h] = at[h] >= 0 ? exp2_of((x[h] - top) * kLog2e) * inv : 0.0f;
+            d[h] = g[h] * p[h];
+        }
+        const float all = lanes_sum<kLanes>(d[0] + d[1]);
+        base[0] = -p[0] * all;
+        base[1] = -p[1] * all;
+        const float by = -all * inv;
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[r][i] *= by;
+            if (mine < a.N) cols.write(out, a.E, r, e[r]);
+        }
     } else {
-        for (int e = lane; e < a.E; e += 32) out[e] = 0.0f;
+        const float zero[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r)
+            if (mine < a.N) cols.write(out, a.E, r, zero);
         float q[2];
-        const float most = warp_max(fmaxf(x[0], x[1]));
+        const float most = lanes_max<kLanes>(fmaxf(x[0], x[1]));
         const bool shift = a.score == TAOT_SOFTMAX || most < -40.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) q[h] = x[h] == -INFINITY ? 0.0f : shift ? expf(x[h] - most) : sigmoid(x[h]);
         if (a.renormalise) {
-            const float sum = fmaxf(warp_sum(q[0] + q[1]), FLT_MIN);
-            q[0] /= sum; q[1] /= sum;
-            const float mean = warp_sum(g[0] * q[0] + g[1] * q[1]);
+            const float inv = 1.0f / fmaxf(lanes_sum<kLanes>(q[0] + q[1]), FLT_MIN);
+            q[0] *= inv; q[1] *= inv;
+            const float mean = lanes_sum<kLanes>(g[0] * q[0] + g[1] * q[1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) d[h] = q[h] * (g[h] - mean);
         } else {
@@ -102,14 +182,42 @@ route_grad_kernel(RouteGradArgs a)
         for (int h = 0; h < 2; ++h)
             if (x[h] == -INFINITY) d[h] = 0.0f;
     }
-    __syncwarp();
+    // an expert that stands in several places: its first place adds them up, in order
+    float sum[2] = {0.0f, 0.0f};
+    bool leads[2] = {at[0] >= 0, at[1] >= 0};
     for (int j = 0; j < a.k; ++j) {
-        const int e = __shfl_sync(kAll, j < 32 ? at[0] : at[1], j & 31);
-        const float v = __shfl_sync(kAll, j < 32 ? d[0] : d[1], j & 31);
-        if (e >= 0 && (e & 31) == lane) out[e] += v;
+        const int from = (lane & ~(kLanes - 1)) | (j & (kLanes - 1));
+        const int e = __shfl_sync(kAll, j < kLanes ? at[0] : at[1], from);
+        const float v = __shfl_sync(kAll, j < kLanes ? d[0] : d[1], from);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (e != at[h]) continue;
+            sum[h] += v;
+            if (j < cols.sub + kLanes * h) leads[h] = false;
+        }
     }
-    __syncwarp();
-    for (int e = lane; e < a.E; e += 32) put(a.dlogits, row * a.ld_out + e, a.dtype, out[e]);
+    __syncwarp();                                  // the row is written before its chosen experts
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (leads[h] && mine < a.N) out[at[h]] = from_f32<T>(base[h] + sum[h]);
+}
+
+template <typename T, int kLanes, int kRuns, bool WIDE>
+cudaError_t launch_grad(const RouteGradArgs& a, cudaStream_t st)
+{
+    constexpr int kRows = kWarps * 32 / kLanes;
+    const unsigned grid = (unsigned)((a.N + kRows - 1) / kRows);
+    if (a.score == TAOT_SOFTMAX && !a.renormalise) route_grad_kernel<T, kLanes, kRuns, WIDE, true><<<grid, kWarps * 32, 0, st>>>(a);
+    else route_grad_kernel<T, kLanes, kRuns, WIDE, false><<<grid, kWarps * 32, 0, st>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, bool WIDE>
+cudaError_t launch_grad(const RouteGradArgs& a, cudaStream_t st)
+{
+    if (a.k <= 16 && a.E <= 64) return launch_grad<T, 8, 1, WIDE>(a, st);
+    if (a.k <= 16 && a.E <= 128) return launch_grad<T, 8, 2, WIDE>(a, st);
+    if (a.k <= 16 && a.E <= 256) return launch_grad<T, 8, 4, WIDE>(a, st);
+    return a.E <= 512 ? launch_grad<T, 32, 2, WIDE>(a, st) : launch_grad<T, 32, 4, WIDE>(a, st);
 }
 
 int check(const taot_route_params* p)
@@ -180,7 +288,10 @@ extern "C" int taot_route_backward(const taot_route_params* p, const void* d_log
     a.logits = d_logits; a.topk = d_topk; a.dweights = d_dweights; a.dlogits = d_dlogits;
     a.N = N; a.ld = p->ld_logits; a.ld_out = p->ld_dlogits; a.scale = p->scale;
     a.E = p->E; a.k = p->k; a.score = p->score; a.renormalise = p->renormalise; a.dtype = p->dtype;
-    route_grad_kernel<<<(unsigned)((N + kWarps - 1) / kWarps), kWarps * 32, sizeof(float) * kWarps * p->E, static_cast<cudaStream_t>(stream)>>>(a);
-    TAOT_CUDA_OK(cudaGetLastError());
+    const bool wide = p->E % 8 == 0 && wide_rows(d_logits, p->ld_logits, e) && wide_rows(d_dlogits, p->ld_dlogits, e);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p->dtype == TAOT_F32) TAOT_CUDA_OK((wide ? launch_grad<float, true>(a, st) : launch_grad<float, false>(a, st)));
+    else if (p->dtype == TAOT_BF16) TAOT_CUDA_OK((wide ? launch_grad<__nv_bfloat16, true>(a, st) : launch_grad<__nv_bfloat16, false>(a, st)));
+    else TAOT_CUDA_OK((wide ? launch_grad<__half, true>(a, st) : launch_grad<__half, false>(a, st)));
     return TAOT_OK;
 }

@@ -209,7 +209,7 @@ __device__ __forceinline__ void grad_rows(const RowsArgs& a, const Part& p, cons
                 widen(row[u], f);
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    if ((WIDE ? c0 + 8 * lane : c0 + 32 * q + lane) < a.D) dot[u] = fmaf(d[q], f[q], dot[u]);
+                    if (column<WIDE, T>(c0, lane, q) < a.D) dot[u] = fmaf(d[q], f[q], dot[u]);
             }
         }
         if (dy)
@@ -238,7 +238,7 @@ __device__ __forceinline__ void grad_rows(const RowsArgs& a, const Part& p, cons
 }
 
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, WIDE && sizeof(T) == 2 ? 3 : 2)
 combine_grad_kernel(RowsArgs a, const T* dout, const T* y, T* dy, float* dweights)
 {
     __shared__ float part[kWarps][8];
@@ -255,12 +255,16 @@ combine_grad_kernel(RowsArgs a, const T* dout, const T* y, T* dy, float* dweight
     if (i < p.entries) grad_rows<1, WIDE>(a, p, dout, y, dy, dweights, i, part);
 }
 
-// A token is shared by as many warps as its rows have 32 runs, so that a row is read and written in pieces as long as may be.  Returns
-// the CTAs.
+// How many warps share a token.  Of many tokens as many as leave at most a fifth of the lanes idle at the row's end, so that a row is
+// read and written in long pieces; of few tokens as many as there is work for.  Returns the CTAs.
+constexpr uint32_t kFewTokens = 592;                   // four CTAs per SM
 unsigned set_share(RowsArgs& a, int64_t runs)
 {
     a.share = 0;
-    while ((1 << a.share) < kWarps && runs > 32 << a.share) ++a.share;
+    for (int s = 1; (1 << s) <= kWarps && runs > 32 << (s - 1); ++s) {
+        const int64_t lanes = (int64_t)32 << s;
+        if (a.tokens <= kFewTokens || (runs + lanes - 1) / lanes * lanes * 4 <= runs * 5) a.share = s;
+    }
     return (unsigned)((((uint64_t)a.tokens << a.share) + kWarps - 1) / kWarps);
 }
 
@@ -339,7 +343,7 @@ extern "C" int taot_send(const taot_rows_params* p, int32_t elem, const void* d_
     a.ld_tokens = p->ld_tokens * elem / word;
     a.ld_rows = p->ld_rows * elem / word;
     a.D = (int32_t)((int64_t)p->D * elem / word);
-    const unsigned grid = set_share(a, a.D);
+    const unsigned grid = set_share(a, a.tokens <= kFewTokens ? a.D : (a.D + 3) / 4);       // (a lane takes four words)
     const auto launch = [&](auto t) {
         typedef decltype(t) W;
         send_kernel<W><<<grid, kThreads, 0, st>>>(a, static_cast<const W*>(d_x), static_cast<W*>(d_rows), d_scales, d_row_scales, cols);
