@@ -54,8 +54,13 @@ struct Row {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v.v[i] = row[min(expert(r, i), E - 1)];
         }
+        // a NaN and what is closed as the lowest value, an infinity as the largest
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = expert(r, i) < E ? seen(to_f32(v.v[i]), Type<T>::big) : -INFINITY;
+        for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(to_f32(v.v[i]), -Type<T>::big), Type<T>::big);
+        if (E != kLanes * 8 * kRuns)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (expert(r, i) >= E) x[i] = -INFINITY;
     }
     __device__ __forceinline__ void write(T* row, int E, int r, const float (&x)[8]) const
     {
@@ -72,14 +77,6 @@ struct Row {
         }
     }
 };
-// 2^v to 2^-22 of itself, down to the smallest values
-__device__ __forceinline__ float exp2_of(float v)
-{
-    float r;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-
 template <int kLanes>
 __device__ __forceinline__ float lanes_max(float v)
 {
@@ -129,25 +126,44 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
             for (int i = 0; i < 8; ++i) top = fmaxf(top, e[r][i]);
         }
         top = lanes_max<kLanes>(top);
-        if (top == -INFINITY) top = 0.0f;          // no open expert: every score is zero
+        // Exponentials relative to the largest, times 2^64, so that small ones stay normal numbers; the factor goes with their
+        // sum's reciprocal.  One multiply-add each: the rounding of top * log2 e is common to the row and goes the same way.
+        // Only where that is no small number, or the lowest value is not far below, the careful form is needed.
+        const bool careful = __any_sync(kAll, fabsf(top) > 65536.0f || top < -0.5f * big);
+        const float shift = 64.0f - top * kLog2e;
+        if (!careful) {
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[r][i] = fast_exp2(fmaf(e[r][i], kLog2e, shift));
+        } else {
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[r][i] = e[r][i] > -big ? fast_exp2(fmaf(e[r][i] - top, kLog2e, 64.0f)) : 0.0f;
+        }
 #pragma unroll
         for (int r = 0; r < kRuns; ++r)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                e[r][i] = exp2_of((e[r][i] - top) * kLog2e);
-                total += e[r][i];
-            }
+            for (int i = 0; i < 8; ++i) total += e[r][i];
         const float inv = 1.0f / fmaxf(lanes_sum<kLanes>(total), FLT_MIN);
         float p[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            p[h] = at[h] >= 0 ? exp2_of((x[h] - top) * kLog2e) * inv : 0.0f;
+            p[h] = x[h] > -INFINITY ? fast_exp2(careful ? fmaf(x[h] - top, kLog2e, 64.0f) : fmaf(x[h], kLog2e, shift)) * inv : 0.0f;
             d[h] = g[h] * p[h];
         }
         const float all = lanes_sum<kLanes>(d[0] + d[1]);
         base[0] = -p[0] * all;
         base[1] = -p[1] * all;
-        const float by = -all * inv;
+        float by = -all * inv;
+        if (const bool tiny = fabsf(all) < 0x1p-60f; __any_sync(kAll, tiny)) {           // then the factor belongs to it
+            by = -(tiny ? all * 0x1p64f : all) * inv;
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[r][i] *= tiny ? 0x1p-64f : 1.0f;
+        }
 #pragma unroll
         for (int r = 0; r < kRuns; ++r) {
 #pragma unroll
@@ -183,17 +199,25 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
             if (x[h] == -INFINITY) d[h] = 0.0f;
     }
     // an expert that stands in several places: its first place adds them up, in order
-    float sum[2] = {0.0f, 0.0f};
-    bool leads[2] = {at[0] >= 0, at[1] >= 0};
-    for (int j = 0; j < a.k; ++j) {
-        const int from = (lane & ~(kLanes - 1)) | (j & (kLanes - 1));
-        const int e = __shfl_sync(kAll, j < kLanes ? at[0] : at[1], from);
-        const float v = __shfl_sync(kAll, j < kLanes ? d[0] : d[1], from);
+    float sum[2] = {d[0], d[1]};
+    bool leads[2] = {at[0] >= 0, at[1] >= 0}, twice = a.k > kLanes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (e != at[h]) continue;
-            sum[h] += v;
-            if (j < cols.sub + kLanes * h) leads[h] = false;
+    for (int o = 1; o < kLanes; ++o) {
+        const int e = __shfl_xor_sync(kAll, at[0], o);
+        twice = twice || (e == at[0] && e >= 0);
+    }
+    if (__any_sync(kAll, twice)) {
+        sum[0] = sum[1] = 0.0f;
+        for (int j = 0; j < a.k; ++j) {
+            const int from = (lane & ~(kLanes - 1)) | (j & (kLanes - 1));
+            const int e = __shfl_sync(kAll, j < kLanes ? at[0] : at[1], from);
+            const float v = __shfl_sync(kAll, j < kLanes ? d[0] : d[1], from);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (e != at[h]) continue;
+                sum[h] += v;
+                if (j < cols.sub + kLanes * h) leads[h] = false;
+            }
         }
     }
     __syncwarp();                                  // the row is written before its chosen experts
