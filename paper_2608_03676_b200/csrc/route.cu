@@ -287,7 +287,8 @@ extern "C" int taot_route(const taot_route_params* p, const void* d_logits, cons
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool lists = p->k <= 16 && (p->groups == 1 || ((p->groups == 2 || p->groups == 4 || p->groups == 8) && p->E % 32 == 0));
     if (lists) {
-        TAOT_CUDA_OK(launch_lanes(a, wide_rows(d_logits, p->ld_logits, e), st));
+        const bool wide = wide_rows(d_logits, p->ld_logits, e);
+        TAOT_CUDA_OK((streams(a, wide) ? launch_stream(a, st) : launch_lanes(a, wide, st)));
     } else {
         route_kernel<<<(unsigned)((N + kWarps - 1) / kWarps), kWarps * 32, sizeof(uint64_t) * kWarps * p->E, st>>>(a);
         TAOT_CUDA_OK(cudaGetLastError());

@@ -515,4 +515,9 @@ __device__ __forceinline__ void four(const __half* p, float (&x)[4])
 // launches the kernels of rows that a warp's lanes share (route_lanes.cu)
 cudaError_t launch_lanes(const RouteArgs& a, bool wide, cudaStream_t st);
 
+// the kernels of rows that a lane has to itself (route_stream.cu), and whether they take a call
+constexpr int64_t kStreamRows = 16384;
+bool streams(const RouteArgs& a, bool wide);
+cudaError_t launch_stream(const RouteArgs& a, cudaStream_t st);
+
 }  // namespace route

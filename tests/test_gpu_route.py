@@ -191,6 +191,86 @@ def test_route_layers_masks_and_strides(E, k, groups):
     assert none["topk"].shape == (L, 0, k) and none["weights"].shape == (L, 0, k)
 
 
+def special_rows(E, dtype, seed):
+    """Rows of every kind that the tests above have: spread, far apart, coarse, next to each other, masked, empty, infinite."""
+    g = torch.Generator().manual_seed(seed)
+    x = 1.5 * torch.randn((60, E), generator=g)
+    x[8:16] = torch.randint(-4, 4, (8, E), generator=g) / 4
+    x[16:24] = 0.5 + 1e-6 * torch.randn((8, E), generator=g) + torch.randint(0, 3, (8, E), generator=g)
+    x[24] = 0.25
+    x[25, ::2] = -0.0
+    x[26:30] *= 40
+    x[30] -= 200
+    x = x.to(dtype)
+    low = torch.finfo(dtype).min
+    x[31] = -INF
+    x[32] = low
+    x[33] = NAN
+    x[34, 3:] = -INF
+    x[35, ::2] = low
+    x[36, 1::2] = NAN
+    x[37, : E - 1] = -INF
+    x[38, 5] = INF
+    x[39, 5] = x[39, 7] = INF
+    x[40, 5] = torch.finfo(dtype).max
+    x[41, 5] = torch.finfo(dtype).max
+    x[41, 7] = INF
+    x[42] = INF
+    x[43] = low / 2
+    x[44, 1:] = low / 2
+    x[45, : E - 2] = low
+    x[46] = x[46].abs()
+    x[47] = -x[47].abs()
+    return x
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,k", [(8, 1), (16, 8), (32, 2), (64, 8), (72, 6), (104, 7), (128, 8), (128, 4), (256, 8), (512, 8), (1024, 8), (40, 3), (256, 12)])
+@pytest.mark.parametrize("score,renormalise", [("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)])
+def test_route_many_rows(dtype, E, k, score, renormalise):
+    """The same rows again and again, in other lanes each time: every copy gets what the definition gives the row."""
+    x = special_rows(E, dtype, seed=E + k)
+    N, times = x.shape[0], 1001
+    kw = dict(score=score, renormalise=renormalise, scale=1.5)
+    topk, w = call(x.repeat(times, 1), k, **kw)
+    check(x, (topk[:N], w[:N]), k, **kw)
+    topk, w = topk.reshape(times, N, k), w.reshape(times, N, k)
+    assert (topk == topk[:1]).all() and (w == w[:1]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,k", [(64, 8), (256, 8), (128, 6)])
+@pytest.mark.parametrize("score,groups,with_bias", [("sigmoid", 8, True), ("softmax", 4, False), ("sigmoid", 1, True), ("softmax", 2, True)])
+def test_route_many_rows_with_bias_and_groups(dtype, E, k, score, groups, with_bias):
+    x = special_rows(E, dtype, seed=E + groups)
+    N, times = x.shape[0], 601
+    bias = 0.1 * torch.randn(E, generator=torch.Generator().manual_seed(E)) if with_bias else None
+    kw = dict(score=score, groups=groups, groups_kept=(groups + 1) // 2, group_top=2, scale=2.5)
+    topk, w = call(x.repeat(times, 1), k, bias=bias, **kw)
+    check(x, (topk[:N], w[:N]), k, bias=None if bias is None else bias.expand(N, -1), **kw)
+    topk, w = topk.reshape(times, N, k), w.reshape(times, N, k)
+    assert (topk == topk[:1]).all() and (w == w[:1]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_route_many_rows_strided_masked_in_layers(dtype):
+    import paper_2608_03676_b200 as P
+    L, T, E, k = 3, 20000, 96, 5
+    x = special_rows(E + 32, dtype, seed=4).repeat(L * T // 60, 1).view(L, T, E + 32).cuda()
+    mask = torch.rand((L, T), generator=torch.Generator().manual_seed(1)) < 0.8
+    for start in (0, 1, 16):
+        part = x[:, :, start:start + E]
+        got = P.route(part, k, mask=mask.cuda())
+        want = P.route(part[0, :60].contiguous(), k)               # (few rows: another kernel)
+        for name, none in (("topk", -1), ("weights", 0)):
+            all_rows = want[name].repeat(L * T // 60, 1).view(L, T, k)
+            all_rows = torch.where(mask.cuda()[..., None], all_rows, torch.full_like(all_rows, none))
+            if name == "topk":
+                assert torch.equal(got[name], all_rows)
+            else:
+                assert torch.allclose(got[name], all_rows, rtol=400 * F32, atol=1e-37)
+
+
 def grad(logits, topk, dw, **kw):
     import paper_2608_03676_b200 as P
     return P.route_backward(logits.cuda(), topk.cuda(), dw.cuda(), **kw).double().cpu().numpy()
