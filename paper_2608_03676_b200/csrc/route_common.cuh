@@ -370,7 +370,7 @@ __device__ __forceinline__ float fast_reciprocal(float v)
 
 // The score of an open logit in fp32, and how far it may be off.  The exponent t is rounded twice, by |t| 2^-24 each.
 //   sigmoid: the exponential is off by 2 |t| 2^-24 ln 2 + 2^-22 of itself, the score by that times s (1 - s) (|t| s (1 - s) stays
-//            below 0.33), and by 2^-23 and 2^-24 of itself: less than 4e-7 in all;
+//            below 0.33, s (1 - s) below 1 / 4), and by 2^-23 and 2^-24 of itself: 2.8e-8 + 6e-8 + 1.8e-7 < 3e-7 in all;
 //   softmax: the same of the exponential, with p |t| below 0.54 p_max; and the sum, in which `terms` terms follow one another.
 struct Scores {
     float top, inv;               // largest logit, reciprocal of the sum of exponentials (softmax)
@@ -382,7 +382,7 @@ __device__ __forceinline__ float score_of(int32_t score, const Scores& s, float 
 }
 __device__ __forceinline__ float score_error(int32_t score, const Scores& s, int terms)
 {
-    return score == TAOT_SIGMOID ? 4e-7f : s.inv * ((float)(terms + 16) * 1.2e-7f);
+    return score == TAOT_SIGMOID ? 3e-7f : s.inv * ((float)(terms + 16) * 1.2e-7f);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -516,7 +516,6 @@ __device__ __forceinline__ void four(const __half* p, float (&x)[4])
 cudaError_t launch_lanes(const RouteArgs& a, bool wide, cudaStream_t st);
 
 // the kernels of rows that a lane has to itself (route_stream.cu), and whether they take a call
-constexpr int64_t kStreamRows = 16384;
 bool streams(const RouteArgs& a, bool wide);
 cudaError_t launch_stream(const RouteArgs& a, cudaStream_t st);
 

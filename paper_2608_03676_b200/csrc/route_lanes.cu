@@ -37,6 +37,25 @@ __device__ __forceinline__ void merge_lanes(uint32_t (&v)[K], uint32_t& lost)
     }
 }
 
+// The lane of a row's eight that has its sub-th place by keys, larger ones first, equal ones by expert; lanes without an expert
+// (-1) have the smallest key and come last.
+__device__ __forceinline__ int lane_of_place(uint64_t key, int at)
+{
+    const int lane = threadIdx.x & 31, sub = lane & (kLanes - 1), base = lane - sub;
+    int rank = 0, from = 0;
+#pragma unroll
+    for (int o = 1; o < kLanes; ++o) {
+        const uint64_t u = __shfl_xor_sync(kAll, key, o);
+        const int e = __shfl_xor_sync(kAll, at, o);
+        const bool before = at < 0 ? e >= 0 || (sub ^ o) < sub : e >= 0 && (u > key || (u == key && e < at));
+        if (before) ++rank;
+    }
+#pragma unroll
+    for (int o = 0; o < kLanes; ++o)
+        if (__shfl_sync(kAll, rank, base + o) == sub) from = o;
+    return base + from;
+}
+
 // the four logits of chunk c, NaN beyond the last expert
 template <typename T, bool WIDE>
 __device__ __forceinline__ void load_chunk(const T* row, int c, int E, float (&x)[4])
@@ -51,7 +70,7 @@ __device__ __forceinline__ void load_chunk(const T* row, int c, int E, float (&x
 // 4, 2 or 1 lanes (E is a multiple of 32).  WIDE: rows of whole chunks that can be read as such.  U: chunks of a lane that
 // are taken at a time (4 where it has no more).
 template <typename T, int K, int U, bool BIAS, bool GROUP, bool WIDE>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, K == 8 ? 6 : 4)
 route_lanes_kernel(const __grid_constant__ RouteArgs a)
 {
     extern __shared__ uint64_t keys[];
@@ -98,36 +117,45 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
 
     // the K best chunks
     uint32_t best[K], lost = 0, bits = 0;
+    float ref = 0.0f;
     float g1 = -INFINITY, g2 = -INFINITY;                          // the two largest keys of the lane's part of its group
     for (int i0 = 0; i0 < per; i0 += U) {
         uint32_t list[K];
 #pragma unroll
         for (int u = 0; u < K; ++u) list[u] = 0;
-        float xs[U][4], bs[BIAS ? U : 1][4];                       // (read before any of them is used)
+        float xs[U][4], m[U];                                      // (read before any of them is used)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u;
             const int c = min(GROUP ? sub * per + i : i * kLanes + sub, C - 1);
             load_chunk<T, WIDE>(x_row, c, a.E, xs[u]);
-            if (BIAS) {
-                if (WIDE) four(b_row + 4 * c, bs[u]);
-                else
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) bs[u][q] = 4 * c + q < a.E ? b_row[4 * c + q] : INFINITY;
-            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u;
             const int c = GROUP ? sub * per + i : i * kLanes + sub;
+            m[u] = -INFINITY;
             if (i >= per || c >= C) continue;
             float (&x)[4] = xs[u];
-            float m;
             if (BIAS) {
-                const float (&b)[4] = bs[u];
+                float b[4];
+                if (WIDE) four(b_row + 4 * c, b);
+                else
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    x[q] = x[q] > -big && fabsf(b[q]) < INFINITY ? score_of(a.score, sc, fminf(x[q], big)) + b[q] : -INFINITY;
+                    for (int q = 0; q < 4; ++q) b[q] = 4 * c + q < a.E ? b_row[4 * c + q] : INFINITY;
+                if (a.score == TAOT_SIGMOID) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {                  // (an infinite logit has score 1 as it is)
+                        const float v = score_of(TAOT_SIGMOID, sc, x[q]) + b[q];
+                        x[q] = x[q] > -big && fabsf(v) < INFINITY ? v : -INFINITY;
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float v = score_of(TAOT_SOFTMAX, sc, fminf(x[q], big)) + b[q];
+                        x[q] = x[q] > -big && fabsf(v) < INFINITY ? v : -INFINITY;
+                    }
+                }
             } else if (GROUP || !kExact) {
                 if (!kExact) bits |= __float_as_uint(x[0]) | __float_as_uint(x[1]) | __float_as_uint(x[2]) | __float_as_uint(x[3]);
 #pragma unroll
@@ -140,9 +168,22 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
                     g1 = fmaxf(g1, x[q]);
                 }
             }
-            m = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-            m = seen(m, big) + 0.0f;                               // (+ 0: one zero)
-            list[u] = m > -INFINITY ? (ordered(m) & ~cmask) | (cmask - (uint32_t)c) : 0u;
+            m[u] = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+            if (!BIAS) m[u] = seen(m[u], big) + 0.0f;              // (+ 0: one zero)
+        }
+        if (!kExact && i0 == 0) {
+            // keys are of the distance to the largest (of the first block), which keeps more of what tells the best apart; not so
+            // where the logits' own bits are fewer than a key's
+            float most = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < U; ++u) most = fmaxf(most, m[u]);
+            most = row_max(most);
+            if (BIAS || (per <= U && (__reduce_or_sync(kAll, bits) & drop) != 0)) ref = most > -INFINITY ? most : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u, c = GROUP ? sub * per + i : i * kLanes + sub;
+            if (m[u] > -INFINITY) list[u] = (ordered(kExact ? m[u] : m[u] - ref) & ~cmask) | (cmask - (uint32_t)c);
         }
         sort_list(list);
         if (i0 == 0) {
@@ -155,9 +196,9 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
     uint64_t* const scratch = keys + (threadIdx.x >> 5) * max(a.E, 16);
     int32_t* const found = reinterpret_cast<int32_t*>(scratch);
     bool redo = false;
-    uint32_t kept_groups = 1u;
+    uint32_t kept_lanes = 1u;                                      // of the row, by its lanes
     if (GROUP) {
-        const int lanes = kLanes / a.groups;                       // of a group
+        const int shift = __ffs(kLanes / a.groups) - 1, lanes = 1 << shift;              // of a group
         for (int o = 1; o < lanes; o *= 2) {
             const float h1 = __shfl_xor_sync(kAll, g1, o), h2 = __shfl_xor_sync(kAll, g2, o);
             g2 = fmaxf(fminf(g1, h1), fmaxf(g2, h2));
@@ -169,13 +210,13 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             s2 = g2 > -INFINITY ? score_of(a.score, sc, g2) : -INFINITY;
         }
         const float score = a.top == 2 && s2 > -INFINITY ? s1 + s2 : s1;
-        const int g = sub / lanes;
+        const int g = sub >> shift;
         int rank = 0;
 #pragma unroll
         for (int o = 1; o < kLanes; ++o) {
             const float other = __shfl_xor_sync(kAll, score, o);
-            const int h = (sub ^ o) / lanes;
-            if (h != g && (sub ^ o) % lanes == 0 && (other > score || (other == score && h < g))) ++rank;
+            const int h = (sub ^ o) >> shift;
+            if (h != g && ((sub ^ o) & (lanes - 1)) == 0 && (other > score || (other == score && h < g))) ++rank;
         }
         bool kept = rank < a.kept;
         const float worst = row_min(kept ? score : INFINITY), next = row_max(kept ? -INFINITY : score);
@@ -194,9 +235,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
                 else redo = true;
             }
         }
-        kept_groups = 0;
-        const unsigned votes = __ballot_sync(kAll, kept) >> (lane & ~(kLanes - 1));
-        for (int h = 0; h < a.groups; ++h) kept_groups |= (votes >> (h * lanes) & 1) << h;
+        kept_lanes = __ballot_sync(kAll, kept) >> (lane & ~(kLanes - 1)) & ((1u << kLanes) - 1);
         if (!kept) {
 #pragma unroll
             for (int i = 0; i < K; ++i) best[i] = 0;
@@ -237,7 +276,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
                 v = v > -INFINITY && fabsf(b) < INFINITY ? score_of(a.score, sc, v) + b : -INFINITY;
             }
             const uint32_t low = kExact ? kLow - (uint32_t)e : kSlots - (uint32_t)(4 * (sub + kLanes * h) + q);
-            list[4 * h + q] = v > -INFINITY ? (ordered(v) & ~(kExact ? kLow : kSlots)) | low : 0u;
+            list[4 * h + q] = v > -INFINITY ? (ordered(kExact ? v : v - ref) & ~(kExact ? kLow : kSlots)) | low : 0u;
         }
     }
     sort_list(list);
@@ -294,18 +333,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
                 const int e_after = __shfl_down_sync(kAll, at[0], 1);
                 const bool turned = sub < kLanes - 1 && e_after >= 0 && (after > v[0] || (after == v[0] && e_after < at[0]));
                 if (__any_sync(kAll, turned)) {
-                    int rank = 0;
-#pragma unroll
-                    for (int o = 1; o < kLanes; ++o) {
-                        const float u = __shfl_xor_sync(kAll, v[0], o);
-                        const int e = __shfl_xor_sync(kAll, at[0], o);
-                        if (u > v[0] || (u == v[0] && ((e < at[0] && e >= 0) || (e == at[0] && (sub ^ o) < sub)))) ++rank;
-                    }
-                    int from = 0;                                  // the lane that has place sub
-#pragma unroll
-                    for (int o = 0; o < kLanes; ++o)
-                        if (__shfl_sync(kAll, rank, (lane & ~(kLanes - 1)) + o) == sub) from = o;
-                    from += lane & ~(kLanes - 1);
+                    const int from = lane_of_place((uint64_t)ordered(v[0]), at[0]);
                     at[0] = __shfl_sync(kAll, at[0], from);
                     x[0] = __shfl_sync(kAll, x[0], from);
                     v[0] = __shfl_sync(kAll, v[0], from);
@@ -327,11 +355,17 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
                 if (wraps && h == kOwn - 1) e = -1;
                 if (e >= 0 && !(v[h] - u > err) && !(x[h] == y && b[h] == c && at[h] < e)) fine = false;
             }
+            if (K == 8 && a.score == TAOT_SIGMOID && __any_sync(kAll, !fine)) {          // the order of the chosen ones in 64 bits
+                const int from = lane_of_place(at[0] >= 0 ? exact_key(a, b_row, true, row, at[0], 0.0f, 1.0) : 0ull, at[0]);
+                at[0] = __shfl_sync(kAll, at[0], from);
+                x[0] = __shfl_sync(kAll, x[0], from);
+                fine = true;
+            }
             least = row_min(fminf(v[0] > -INFINITY ? v[0] : INFINITY, v[kOwn - 1] > -INFINITY ? v[kOwn - 1] : INFINITY));
-            if (beyond != 0 && !(least > number_of(beyond | drop) + err)) fine = false;
+            if (beyond != 0 && !(least - ref > number_of(beyond | drop) + err)) fine = false;
             least -= err;
         } else if (!lossless) {
-            least = last ? number_of(last & ~drop) : -INFINITY;
+            least = row_min(fminf(x[0] > -INFINITY ? x[0] : INFINITY, x[kOwn - 1] > -INFINITY ? x[kOwn - 1] : INFINITY));
             if (beyond != 0 && ((beyond ^ last) & ~drop) == 0) fine = false;
             if (K == 8) {
                 const float after = __shfl_down_sync(kAll, x[0], 1);
@@ -381,7 +415,12 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             const int64_t r = first + from / kLanes;
             const Scores s = {__shfl_sync(kAll, sc.top, from), __shfl_sync(kAll, sc.inv, from)};
             const float limit = __shfl_sync(kAll, least, from);
-            const uint32_t groups = __shfl_sync(kAll, kept_groups, from);
+            const uint32_t lanes_kept = __shfl_sync(kAll, kept_lanes, from);
+            uint32_t groups = 1u;
+            if (GROUP) {
+                groups = 0;
+                for (int g = 0, each = kLanes / a.groups; g < a.groups; ++g) groups |= (lanes_kept >> (g * each) & 1u) << g;
+            }
             int at0 = -1, at1 = -1;
             float t = s.top, z = __shfl_sync(kAll, total, from);
             if (__shfl_sync(kAll, (int)redo, from) || !settle_choice(a, r, s, groups, limit, found, at0))

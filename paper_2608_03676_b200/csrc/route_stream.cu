@@ -335,10 +335,15 @@ cudaError_t launch(const RouteArgs& a, cudaStream_t st)
 
 }  // namespace
 
+// Against eight lanes per row, us:   rows of 256 B (128 bf16, 64 fp32)  32768: 6.1 : 8.0, 8.5 : 12.4    2^20: 81 : 198
+//                                     512 B (256 bf16, 128 fp32)        16384: 7.5 : 5.7, 10.2 : 8.7    65536: 17.9 : 17.6, 19.4 : 24.3
+//                                                                       262144: 46 : 63, 50 : 84
+//                                     1 KB (512 bf16, 256 fp32)         131072: 56 : 46,  262144: 104 : 104
+// With long rows too few warps fit in shared memory, with few rows there are too few warps.
 bool streams(const RouteArgs& a, bool wide)
 {
     const int64_t bytes = (int64_t)a.E * layer::type_bytes(a.dtype);
-    return wide && !a.bias && a.groups == 1 && a.k <= K && bytes % 16 == 0 && bytes <= 2048 && a.N >= kStreamRows;
+    return wide && !a.bias && a.groups == 1 && a.k <= K && bytes % 16 == 0 && bytes <= 512 && a.N >= 128 * bytes;
 }
 
 cudaError_t launch_stream(const RouteArgs& a, cudaStream_t st)

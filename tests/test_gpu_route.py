@@ -167,6 +167,15 @@ def test_route_far_logits(dtype, score, renormalise):
     check(x, call(x, k, bias=bias, **kw), k, bias=bias.expand(N, -1), **kw)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shift", [-1e5, 1e5, -1e30, 1e38])
+def test_route_biases_beyond_the_logits_type(dtype, shift):
+    """Biases are fp32 whatever the logits' type: keys far outside it are keys like others."""
+    x = make(20, 64, dtype, seed=2)
+    bias = shift * (1 + torch.linspace(0, 1, 64))
+    check(x, call(x, 6, bias=bias, score="sigmoid"), 6, bias=bias.expand(20, -1), score="sigmoid")
+
+
 @pytest.mark.parametrize("E,k,groups", [(64, 6, 1), (256, 8, 8)])
 def test_route_layers_masks_and_strides(E, k, groups):
     import paper_2608_03676_b200 as P
@@ -230,7 +239,7 @@ def special_rows(E, dtype, seed):
 def test_route_many_rows(dtype, E, k, score, renormalise):
     """The same rows again and again, in other lanes each time: every copy gets what the definition gives the row."""
     x = special_rows(E, dtype, seed=E + k)
-    N, times = x.shape[0], 1001
+    N, times = x.shape[0], 1101
     kw = dict(score=score, renormalise=renormalise, scale=1.5)
     topk, w = call(x.repeat(times, 1), k, **kw)
     check(x, (topk[:N], w[:N]), k, **kw)
