@@ -56,24 +56,47 @@ __device__ __forceinline__ int lane_of_place(uint64_t key, int at)
     return base + from;
 }
 
-// the four logits of chunk c, NaN beyond the last expert
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load_chunk(const T* row, int c, int E, float (&x)[4])
+__device__ __forceinline__ void copy_async(void* to, const void* from)
 {
-    if (WIDE) four(row + 4 * c, x);
-    else
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = 4 * c + i < E ? to_f32(row[4 * c + i]) : __int_as_float(0x7fc00000);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
+
+// A row's logits: in memory (WIDE: rows of whole chunks, 16-byte aligned), or STAGED in shared memory, to which the warp has brought
+// it: where a lane's chunks follow one another, the lanes of a load would be far apart in memory.  There a lane's own
+// chunks are one 16-byte piece further from the next lane's than they would be, so that the lanes read different banks: piece p
+// stands at p + (p * spread >> 16).
+template <typename T, bool WIDE, bool STAGED>
+struct Logits {
+    const T* row;
+    const uint4* tile;
+    uint32_t spread;
+    int E;
+    __device__ __forceinline__ const T* at(int e) const
+    {
+        if (!STAGED) return row + e;
+        constexpr int kPiece = 16 / (int)sizeof(T);
+        const uint32_t p = (uint32_t)e / kPiece;
+        return reinterpret_cast<const T*>(tile + p + (p * spread >> 16)) + e % kPiece;
+    }
+    // the four logits of chunk c, NaN beyond the last expert
+    __device__ __forceinline__ void chunk(int c, float (&x)[4]) const
+    {
+        if (WIDE) four(at(4 * c), x);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = 4 * c + i < E ? to_f32(row[4 * c + i]) : __int_as_float(0x7fc00000);
+    }
+};
 
 // BIAS: keys are scores with a bias added.  GROUP: 2, 4 or 8 groups; a lane's chunks follow one another, so that a group lies in
 // 4, 2 or 1 lanes (E is a multiple of 32).  WIDE: rows of whole chunks that can be read as such.  U: chunks of a lane that
 // are taken at a time (4 where it has no more).
 template <typename T, int K, int U, bool BIAS, bool GROUP, bool WIDE>
 __global__ void __launch_bounds__(kWarps * 32, K == 8 ? 6 : 4)
-route_lanes_kernel(const __grid_constant__ RouteArgs a)
+route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t pitch, int32_t warp_bytes)
 {
-    extern __shared__ uint64_t keys[];
+    constexpr bool STAGED = WIDE && GROUP;         // (without groups 65536 x 256 bf16 take 17.6 us from memory, 19 staged)
+    extern __shared__ uint4 shared[];
     constexpr int kOwn = K / kLanes;                               // places of the list that a lane stands for
     constexpr uint32_t kSlots = 4 * K - 1;
     constexpr bool kExact = !BIAS && sizeof(T) == 2;               // keys lose nothing
@@ -85,20 +108,37 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
     const int64_t mine = first + lane / kLanes;
     const int64_t row = mine < a.N ? mine : a.N - 1;               // (lanes past the end repeat the last row and write nothing)
     const bool routed = mine < a.N && (!a.mask || a.mask[row]);
-    const T* x_row = static_cast<const T*>(a.logits) + row * a.ld;
+    // the warp's shared memory: a list of experts, then its rows; the latter's place serves choose_exactly at the end
+    int32_t* const found = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(shared) + (threadIdx.x >> 5) * warp_bytes);
+    uint4* const tile = reinterpret_cast<uint4*>(found + 32);
+    if (STAGED) {
+        const int pieces = a.E * (int)sizeof(T) / 16;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int64_t from = min(first + r, a.N - 1);
+            const char* p = reinterpret_cast<const char*>(static_cast<const T*>(a.logits) + from * a.ld);
+            for (int c = lane; c < pieces; c += 32) copy_async(tile + r * pitch + c + ((uint32_t)c * spread >> 16), p + 16 * c);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    const Logits<T, WIDE, STAGED> logits = {static_cast<const T*>(a.logits) + row * a.ld, tile + lane / kLanes * pitch, spread, a.E};
     const float* b_row = BIAS ? a.bias + row / a.T * a.E : nullptr;
     const int C = (a.E + 3) / 4;
     const int per = (C + kLanes - 1) / kLanes;                     // chunks of a lane
     const uint32_t cmask = (1u << a.chunk_bits) - 1;
     const uint32_t drop = max(cmask, kSlots);                      // the bits of a key that are no value
 
+    if (STAGED) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
     Scores sc = {0.0f, 1.0f};
     float total = 1.0f;
     if (a.score == TAOT_SOFTMAX && (BIAS || GROUP || (!a.renormalise && a.weights))) {
         float top = -big;
         for (int c = sub; c < C; c += kLanes) {
             float x[4];
-            load_chunk<T, WIDE>(x_row, c, a.E, x);
+            logits.chunk(c, x);
 #pragma unroll
             for (int q = 0; q < 4; ++q) top = fmaxf(top, x[q]);
         }
@@ -106,7 +146,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
         total = 0.0f;
         for (int c = sub; c < C; c += kLanes) {
             float x[4];
-            load_chunk<T, WIDE>(x_row, c, a.E, x);
+            logits.chunk(c, x);
 #pragma unroll
             for (int q = 0; q < 4; ++q) total += x[q] > -big ? fast_exp2((fminf(x[q], big) - top) * kLog2e) : 0.0f;
         }
@@ -123,20 +163,21 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
         uint32_t list[K];
 #pragma unroll
         for (int u = 0; u < K; ++u) list[u] = 0;
-        float xs[U][4], m[U];                                      // (read before any of them is used)
+        float xs[STAGED ? 1 : U][4], m[U];                           // (read from memory before any of them is used)
+        if (!STAGED)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u;
-            const int c = min(GROUP ? sub * per + i : i * kLanes + sub, C - 1);
-            load_chunk<T, WIDE>(x_row, c, a.E, xs[u]);
-        }
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u;
+                logits.chunk(min(GROUP ? sub * per + i : i * kLanes + sub, C - 1), xs[STAGED ? 0 : u]);
+            }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u;
             const int c = GROUP ? sub * per + i : i * kLanes + sub;
             m[u] = -INFINITY;
             if (i >= per || c >= C) continue;
-            float (&x)[4] = xs[u];
+            float (&x)[4] = xs[STAGED ? 0 : u];
+            if (STAGED) logits.chunk(c, x);
             if (BIAS) {
                 float b[4];
                 if (WIDE) four(b_row + 4 * c, b);
@@ -193,8 +234,6 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             merge_list<!kExact>(best, list, lost);
         }
     }
-    uint64_t* const scratch = keys + (threadIdx.x >> 5) * max(a.E, 16);
-    int32_t* const found = reinterpret_cast<int32_t*>(scratch);
     bool redo = false;
     uint32_t kept_lanes = 1u;                                      // of the row, by its lanes
     if (GROUP) {
@@ -266,7 +305,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
     for (int h = 0; h < kOwn; ++h) {
         if (id[h] >= C) continue;
         float x[4];
-        load_chunk<T, WIDE>(x_row, id[h], a.E, x);
+        logits.chunk(id[h], x);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int e = 4 * id[h] + q;
@@ -304,7 +343,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             }
             at[h] = there ? 4 * chunk + (slot & 3) : -1;
         }
-        x[h] = there ? seen(to_f32(x_row[at[h]]), big) : -INFINITY;
+        x[h] = there ? seen(to_f32(*logits.at(at[h])), big) : -INFINITY;
         v[h] = x[h];
     }
     bool settle = false;
@@ -409,7 +448,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             if (a.weights) a.weights[row * a.k + sub + kLanes * h] = a.scale * w[h];
         }
     if (BIAS || GROUP || !kExact) {
-        for (unsigned left = __ballot_sync(kAll, settle || redo); left;) {
+        for (unsigned left = __ballot_sync(kAll, settle || redo); left;) {             // (all lanes are done with the rows)
             const int from = (__ffs(left) - 1) & ~(kLanes - 1);
             left &= ~(((1u << kLanes) - 1) << from);
             const int64_t r = first + from / kLanes;
@@ -424,7 +463,7 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a)
             int at0 = -1, at1 = -1;
             float t = s.top, z = __shfl_sync(kAll, total, from);
             if (__shfl_sync(kAll, (int)redo, from) || !settle_choice(a, r, s, groups, limit, found, at0))
-                choose_exactly(a, r, scratch, at0, at1, t, z);
+                choose_exactly(a, r, reinterpret_cast<uint64_t*>(tile), at0, at1, t, z);
             write_row(a, r, at0, at1, t, z);
         }
     }
@@ -434,15 +473,24 @@ template <typename T, int K, int U, bool WIDE>
 cudaError_t launch(const RouteArgs& a, cudaStream_t st)
 {
     const unsigned grid = (unsigned)((a.N + kWarps * kRows - 1) / (kWarps * kRows));
-    const size_t scratch = sizeof(uint64_t) * kWarps * (a.E > 16 ? a.E : 16);
-    if (a.groups > 1) {
-        if (a.bias) route_lanes_kernel<T, K, U, true, true, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
-        else route_lanes_kernel<T, K, U, false, true, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
-    } else {
-        if (a.bias) route_lanes_kernel<T, K, U, true, false, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
-        else route_lanes_kernel<T, K, U, false, false, WIDE><<<grid, kWarps * 32, scratch, st>>>(a);
-    }
-    return cudaGetLastError();
+    const int32_t pieces = a.E * (int32_t)sizeof(T) / 16, chunks = (a.E + 3) / 4;
+    // a lane's pieces, where its chunks follow one another and are whole pieces
+    const int32_t own = a.groups > 1 && chunks % kLanes == 0 ? chunks / kLanes * 4 * (int32_t)sizeof(T) : 0;
+    const uint32_t spread = WIDE && own > 0 && own % 16 == 0 ? (65536u + own / 16 - 1) / (own / 16) : 0u;      // (exact for up to 256 pieces)
+    const int32_t pitch = WIDE && a.groups > 1 ? pieces + (spread ? kLanes : 0) : 0;
+    const size_t tile = (size_t)kRows * pitch * 16, exact = sizeof(uint64_t) * (size_t)a.E;
+    const int32_t warp_bytes = (int32_t)(128 + ((tile > exact ? tile : exact) + 15) / 16 * 16);
+    const size_t smem = (size_t)warp_bytes * kWarps;
+    const auto run = [&](auto kernel) {
+        if (smem > 48 * 1024) {
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+        }
+        kernel<<<grid, kWarps * 32, smem, st>>>(a, spread, pitch, warp_bytes);
+        return cudaGetLastError();
+    };
+    if (a.groups > 1) return a.bias ? run(route_lanes_kernel<T, K, U, true, true, WIDE>) : run(route_lanes_kernel<T, K, U, false, true, WIDE>);
+    return a.bias ? run(route_lanes_kernel<T, K, U, true, false, WIDE>) : run(route_lanes_kernel<T, K, U, false, false, WIDE>);
 }
 
 template <typename T>
@@ -457,7 +505,7 @@ cudaError_t by_shape(const RouteArgs& a, bool wide, cudaStream_t st)
 
 cudaError_t launch_lanes(const RouteArgs& a, bool wide, cudaStream_t st)
 {
-    wide = wide && a.E % 4 == 0 && !misaligned(a.bias, 16);
+    wide = wide && a.E * layer::type_bytes(a.dtype) % 16 == 0 && !misaligned(a.bias, 16);
     if (a.dtype == TAOT_F32) return by_shape<float>(a, wide, st);
     if (a.dtype == TAOT_BF16) return by_shape<__nv_bfloat16>(a, wide, st);
     return by_shape<__half>(a, wide, st);
