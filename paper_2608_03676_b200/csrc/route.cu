@@ -282,10 +282,13 @@ extern "C" int taot_route(const taot_route_params* p, const void* d_logits, cons
     a.N = N; a.T = p->T; a.ld = p->ld_logits; a.scale = p->scale;
     a.E = p->E; a.k = p->k; a.score = p->score; a.groups = p->groups; a.kept = p->groups_kept; a.top = p->group_top;
     a.renormalise = p->renormalise; a.dtype = p->dtype;
+    if (a.kept == a.groups) a.groups = a.kept = 1;         // all groups stay
+    // chunks of four experts, which with groups may end inside a chunk of each of the eight lanes
+    const int32_t chunks = a.groups == 1 || p->E % 32 == 0 ? (p->E + 3) / 4 : p->E / 4 + 12;
     a.chunk_bits = 1;
-    while ((1 << a.chunk_bits) <= (p->E + 3) / 4) ++a.chunk_bits;
+    while ((1 << a.chunk_bits) <= chunks) ++a.chunk_bits;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool lists = p->k <= 16 && (p->groups == 1 || ((p->groups == 2 || p->groups == 4 || p->groups == 8) && p->E % 32 == 0));
+    const bool lists = p->k <= 16 && (a.groups == 1 || a.groups == 2 || a.groups == 4 || a.groups == 8);
     if (lists) {
         const bool wide = wide_rows(d_logits, p->ld_logits, e);
         TAOT_CUDA_OK((streams(a, wide) ? launch_stream(a, st) : launch_lanes(a, wide, st)));

@@ -78,19 +78,19 @@ struct Logits {
         const uint32_t p = (uint32_t)e / kPiece;
         return reinterpret_cast<const T*>(tile + p + (p * spread >> 16)) + e % kPiece;
     }
-    // the four logits of chunk c, NaN beyond the last expert
-    __device__ __forceinline__ void chunk(int c, float (&x)[4]) const
+    // four logits from expert e on, NaN from `end` on
+    __device__ __forceinline__ void chunk(int e, int end, float (&x)[4]) const
     {
-        if (WIDE) four(at(4 * c), x);
+        if (WIDE) four(at(e), x);
         else
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = 4 * c + i < E ? to_f32(row[4 * c + i]) : __int_as_float(0x7fc00000);
+            for (int i = 0; i < 4; ++i) x[i] = e + i < end ? to_f32(row[e + i]) : __int_as_float(0x7fc00000);
     }
 };
 
 // BIAS: keys are scores with a bias added.  GROUP: 2, 4 or 8 groups; a lane's chunks follow one another, so that a group lies in
-// 4, 2 or 1 lanes (E is a multiple of 32).  WIDE: rows of whole chunks that can be read as such.  U: chunks of a lane that
-// are taken at a time (4 where it has no more).
+// 4, 2 or 1 lanes.  WIDE: rows of whole chunks that can be read as such (and with groups whole chunks in every lane).  U: chunks
+// of a lane that are taken at a time (4 where it has no more).
 template <typename T, int K, int U, bool BIAS, bool GROUP, bool WIDE>
 __global__ void __launch_bounds__(kWarps * 32, K == 8 ? 6 : 4)
 route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t pitch, int32_t warp_bytes)
@@ -123,8 +123,19 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
     }
     const Logits<T, WIDE, STAGED> logits = {static_cast<const T*>(a.logits) + row * a.ld, tile + lane / kLanes * pitch, spread, a.E};
     const float* b_row = BIAS ? a.bias + row / a.T * a.E : nullptr;
-    const int C = (a.E + 3) / 4;
-    const int per = (C + kLanes - 1) / kLanes;                     // chunks of a lane
+    constexpr bool CUT = GROUP && !WIDE;                           // a lane's part of its group may be any number of experts
+    const int shift = GROUP ? __ffs(kLanes / a.groups) - 1 : 0, lanes = 1 << shift;       // of a group
+    const int size = CUT ? a.E / a.groups : 0, part = CUT ? (size + lanes - 1) >> shift : 0;
+    const int per = CUT ? (part + 3) / 4 : ((a.E + 3) / 4 + kLanes - 1) / kLanes;         // chunks of a lane
+    const int C = CUT ? per * kLanes : (a.E + 3) / 4;
+    // where chunk i of lane s, or chunk c, begins, and where that lane's (or the row's) experts end
+    const auto begin = [&](int s, int i) { return (s >> shift) * size + (s & (lanes - 1)) * part + 4 * i; };
+    const auto end = [&](int s) { return min((s >> shift) * size + ((s & (lanes - 1)) + 1) * part, ((s >> shift) + 1) * size); };
+    const auto chunk = [&](int c, int& e, int& stop) {
+        const int s = CUT ? c / per : 0;
+        e = CUT ? begin(s, c - s * per) : 4 * c;
+        stop = CUT ? end(s) : a.E;
+    };
     const uint32_t cmask = (1u << a.chunk_bits) - 1;
     const uint32_t drop = max(cmask, kSlots);                      // the bits of a key that are no value
 
@@ -136,17 +147,17 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
     float total = 1.0f;
     if (a.score == TAOT_SOFTMAX && (BIAS || GROUP || (!a.renormalise && a.weights))) {
         float top = -big;
-        for (int c = sub; c < C; c += kLanes) {
+        for (int e = 4 * sub; e < a.E; e += 4 * kLanes) {
             float x[4];
-            logits.chunk(c, x);
+            logits.chunk(e, a.E, x);
 #pragma unroll
             for (int q = 0; q < 4; ++q) top = fmaxf(top, x[q]);
         }
         sc.top = top = fminf(row_max(top), big);
         total = 0.0f;
-        for (int c = sub; c < C; c += kLanes) {
+        for (int e = 4 * sub; e < a.E; e += 4 * kLanes) {
             float x[4];
-            logits.chunk(c, x);
+            logits.chunk(e, a.E, x);
 #pragma unroll
             for (int q = 0; q < 4; ++q) total += x[q] > -big ? fast_exp2((fminf(x[q], big) - top) * kLog2e) : 0.0f;
         }
@@ -168,7 +179,8 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u;
-                logits.chunk(min(GROUP ? sub * per + i : i * kLanes + sub, C - 1), xs[STAGED ? 0 : u]);
+                const int c = min(GROUP ? sub * per + i : i * kLanes + sub, C - 1);
+                logits.chunk(CUT ? begin(sub, i) : 4 * c, CUT ? end(sub) : a.E, xs[STAGED ? 0 : u]);
             }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -177,13 +189,14 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
             m[u] = -INFINITY;
             if (i >= per || c >= C) continue;
             float (&x)[4] = xs[STAGED ? 0 : u];
-            if (STAGED) logits.chunk(c, x);
+            if (STAGED) logits.chunk(4 * c, a.E, x);
+            const int e = CUT ? begin(sub, i) : 4 * c, stop = CUT ? end(sub) : a.E;
             if (BIAS) {
                 float b[4];
-                if (WIDE) four(b_row + 4 * c, b);
+                if (WIDE) four(b_row + e, b);
                 else
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) b[q] = 4 * c + q < a.E ? b_row[4 * c + q] : INFINITY;
+                    for (int q = 0; q < 4; ++q) b[q] = e + q < stop ? b_row[e + q] : INFINITY;
                 if (a.score == TAOT_SIGMOID) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {                  // (an infinite logit has score 1 as it is)
@@ -237,7 +250,6 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
     bool redo = false;
     uint32_t kept_lanes = 1u;                                      // of the row, by its lanes
     if (GROUP) {
-        const int shift = __ffs(kLanes / a.groups) - 1, lanes = 1 << shift;              // of a group
         for (int o = 1; o < lanes; o *= 2) {
             const float h1 = __shfl_xor_sync(kAll, g1, o), h2 = __shfl_xor_sync(kAll, g2, o);
             g2 = fmaxf(fminf(g1, h1), fmaxf(g2, h2));
@@ -305,13 +317,15 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
     for (int h = 0; h < kOwn; ++h) {
         if (id[h] >= C) continue;
         float x[4];
-        logits.chunk(id[h], x);
+        int e0, stop;
+        chunk(id[h], e0, stop);
+        logits.chunk(e0, stop, x);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int e = 4 * id[h] + q;
+            const int e = e0 + q;
             float v = seen(x[q], big) + 0.0f;
             if (BIAS) {
-                const float b = WIDE || e < a.E ? b_row[e] : INFINITY;
+                const float b = WIDE || e < stop ? b_row[e] : INFINITY;
                 v = v > -INFINITY && fabsf(b) < INFINITY ? score_of(a.score, sc, v) + b : -INFINITY;
             }
             const uint32_t low = kExact ? kLow - (uint32_t)e : kSlots - (uint32_t)(4 * (sub + kLanes * h) + q);
@@ -336,12 +350,14 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
         } else {
             const int slot = (int)(kSlots - (key & kSlots));
             const int from = (lane & ~(kLanes - 1)) | ((slot >> 2) & (kLanes - 1));
-            int chunk = __shfl_sync(kAll, id[0], from);
+            int number = __shfl_sync(kAll, id[0], from);
             if constexpr (kOwn > 1) {
                 const int other = __shfl_sync(kAll, id[1], from);
-                if (slot >> 5) chunk = other;
+                if (slot >> 5) number = other;
             }
-            at[h] = there ? 4 * chunk + (slot & 3) : -1;
+            int e0, stop;
+            chunk(number, e0, stop);
+            at[h] = there ? e0 + (slot & 3) : -1;
         }
         x[h] = there ? seen(to_f32(*logits.at(at[h])), big) : -INFINITY;
         v[h] = x[h];
@@ -505,7 +521,7 @@ cudaError_t by_shape(const RouteArgs& a, bool wide, cudaStream_t st)
 
 cudaError_t launch_lanes(const RouteArgs& a, bool wide, cudaStream_t st)
 {
-    wide = wide && a.E * layer::type_bytes(a.dtype) % 16 == 0 && !misaligned(a.bias, 16);
+    wide = wide && a.E * layer::type_bytes(a.dtype) % 16 == 0 && !misaligned(a.bias, 16) && (a.groups == 1 || a.E % 32 == 0);
     if (a.dtype == TAOT_F32) return by_shape<float>(a, wide, st);
     if (a.dtype == TAOT_BF16) return by_shape<__nv_bfloat16>(a, wide, st);
     return by_shape<__half>(a, wide, st);

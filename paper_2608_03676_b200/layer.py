@@ -42,8 +42,32 @@ class RowsParams(ctypes.Structure):
                 ("ld_rows", ctypes.c_int64), ("ld_tokens", ctypes.c_int64), ("ld_residual", ctypes.c_int64)]
 
 
+_P, _I = ctypes.c_void_p, ctypes.c_int32
+_ARGS = {                                        # behind the pointer to the params; the stream comes last
+    "taot_rms_norm": [_P] * 8, "taot_rms_norm_backward": [_P] * 8, "taot_route": [_P] * 5, "taot_route_backward": [_P] * 4,
+    "taot_send": [_I, _P, _P, _I, _P, _P, _P, _P, _P], "taot_combine": [_P] * 7, "taot_combine_backward": [_P] * 8,
+}
+_functions: Dict[str, object] = {}
+
+
+def _function(name: str):
+    fn = _functions.get(name)
+    if fn is None:
+        lib = load_library()
+        proto = ctypes.CFUNCTYPE(ctypes.c_int, _P, *_ARGS[name], _P)
+        fn = _functions[name] = proto((name, lib))
+    return fn
+
+
+def _stream_of(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_of)      # the same without a stream object, which takes microseconds
+
+
 def _at(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _type(t: torch.Tensor, name: str) -> int:
@@ -55,10 +79,10 @@ def _type(t: torch.Tensor, name: str) -> int:
 
 def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> int:
     """Checks a tensor whose last dimension is a row; returns the distance between rows in elements."""
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.shape != shape or t.dtype != dtype or t.device != device:
         raise TaotError(f"{name}: expected a tensor {list(shape)} of {dtype} on {device}, not {list(t.shape)} of {t.dtype} on {t.device}")
     if t.is_contiguous():
-        return t.shape[-1]
+        return shape[-1]
     stride = t.stride()
     if t.shape[-1] > 1 and stride[-1] != 1:
         raise TaotError(f"{name}: the columns of a row must be dense")
@@ -78,7 +102,7 @@ def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> int:
 
 
 def _dense(t: Optional[torch.Tensor], name: str, shape, dtype, device):
-    if t is not None and (t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+    if t is not None and (t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous()):
         raise TaotError(f"{name}: expected a contiguous tensor {list(shape)} of {dtype} on {device}")
 
 
@@ -90,15 +114,16 @@ def _start(t: torch.Tensor, name: str, dims: int) -> torch.device:
     return t.device
 
 
-def _call(device: torch.device, what: str, *args):
+def _call(device: torch.device, what: str, params, *args):
     """Calls an entry point with the device's current stream as its last argument, that device being current."""
-    fn = getattr(load_library(), what)
+    fn = _functions.get(what) or _function(what)
     if device.index == torch.cuda.current_device():
-        rc = fn(*args, ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream))
+        rc = fn(ctypes.addressof(params), *args, _stream_of(device.index))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream))
-    _check(rc, what)
+            rc = fn(ctypes.addressof(params), *args, _stream_of(device.index))
+    if rc:
+        _check(rc, what)
 
 
 def _count(shape) -> int:
@@ -126,7 +151,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
     out may hold x or residual as "h", and x as "y"."""
     dev = _start(x, "x", 1)
     D = x.shape[-1]
-    lead = tuple(x.shape[:-1])
+    lead = x.shape[:-1]
     if not want_y and not group:
         raise TaotError("rms_norm: nothing to write (want_y is False and group is 0)")
     code = _type(x, "x")
@@ -148,7 +173,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
         res["scales"] = _slot(out, "scales", cols, torch.float32, dev)
         p.ld_q = _rows(res["q"], "q", x.shape, torch.float8_e4m3fn, dev)
         _dense(res["scales"], "scales", cols, torch.float32, dev)
-    _call(dev, "taot_rms_norm", ctypes.byref(p), _at(x), _at(residual), _at(weight), _at(res.get("h")), _at(res.get("y")),
+    _call(dev, "taot_rms_norm", p, _at(x), _at(residual), _at(weight), _at(res.get("h")), _at(res.get("y")),
           _at(res.get("q")), _at(res.get("scales")), _at(res["rstd"]))
     return res
 
@@ -160,7 +185,7 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
     h: the call's h, or x where it had no residual; dh: what reaches h from elsewhere.  out may hold dy or dh as "dx"."""
     dev = _start(h, "h", 1)
     D = h.shape[-1]
-    lead = tuple(h.shape[:-1])
+    lead = h.shape[:-1]
     code = _type(h, "h")
     _dense(weight, "weight", (D,), h.dtype, dev)
     _dense(rstd, "rstd", lead, torch.float32, dev)
@@ -178,7 +203,7 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
         n = ctypes.c_size_t()
         _check(load_library().taot_rms_norm_backward_workspace(ctypes.byref(p), ctypes.byref(n)), "taot_rms_norm_backward_workspace")
         ws = torch.empty(n.value, dtype=torch.uint8, device=dev)     # of this call alone: its stream's allocator takes it back
-    _call(dev, "taot_rms_norm_backward", ctypes.byref(p), _at(dy), _at(dh), _at(h), _at(weight), _at(rstd), _at(res["dx"]),
+    _call(dev, "taot_rms_norm_backward", p, _at(dy), _at(dh), _at(h), _at(weight), _at(rstd), _at(res["dx"]),
           _at(res.get("dweight")), _at(ws))
     return res
 
@@ -191,7 +216,7 @@ def _route_params(logits: torch.Tensor, k: int, score: str, renormalise: bool, s
     code = _type(logits, "logits")
     if score not in _SCORES:
         raise TaotError(f"score: expected one of {sorted(_SCORES)}, not {score!r}")
-    lead = tuple(logits.shape[:-1])
+    lead = logits.shape[:-1]
     T = lead[-1]
     L = _count(lead[:-1])
     p = RouteParams(ctypes.sizeof(RouteParams), code, L, T, logits.shape[-1], k, _SCORES[score], 1, 1, 1, int(bool(renormalise)), scale)
@@ -221,7 +246,7 @@ def route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optional[t
     if want_weights:
         res["weights"] = _slot(out, "weights", shape, torch.float32, dev)
         _dense(res["weights"], "weights", shape, torch.float32, dev)
-    _call(dev, "taot_route", ctypes.byref(p), _at(logits), _at(bias), _at(mask), _at(res["topk"]), _at(res.get("weights")))
+    _call(dev, "taot_route", p, _at(logits), _at(bias), _at(mask), _at(res["topk"]), _at(res.get("weights")))
     return res
 
 
@@ -236,7 +261,7 @@ def route_backward(logits: torch.Tensor, topk: torch.Tensor, dweights: torch.Ten
     _dense(dweights, "dweights", lead + (p.k,), torch.float32, dev)
     res = torch.empty(logits.shape, dtype=logits.dtype, device=dev) if out is None else out
     p.ld_dlogits = _rows(res, "out", logits.shape, logits.dtype, dev)
-    _call(dev, "taot_route_backward", ctypes.byref(p), _at(logits), _at(topk), _at(dweights), _at(res))
+    _call(dev, "taot_route_backward", p, _at(logits), _at(topk), _at(dweights), _at(res))
     return res
 
 
@@ -290,7 +315,7 @@ def send(x: torch.Tensor, perm: torch.Tensor, counts: Optional[torch.Tensor] = N
         _dense(scales, "scales", lead + (n, cols), torch.float32, dev)
         res["scales"] = _slot(out, "scales", lead + (n * k, cols), torch.float32, dev)
         _dense(res["scales"], "scales", lead + (n * k, cols), torch.float32, dev)
-    _call(dev, "taot_send", ctypes.byref(p), ctypes.c_int32(x.element_size()), _at(x), _at(scales), ctypes.c_int32(cols), _at(perm),
+    _call(dev, "taot_send", p, x.element_size(), _at(x), _at(scales), cols, _at(perm),
           _at(counts), _at(res["rows"]), _at(res.get("scales")), _at(res["info"]))
     return res
 
@@ -309,7 +334,7 @@ def combine(y: torch.Tensor, perm: torch.Tensor, weights: Optional[torch.Tensor]
         p.ld_residual = _rows(residual, "residual", shape, y.dtype, dev)
     res = dict(out=_slot(out, "out", shape, y.dtype, dev), info=_info(out, lead, dev))
     p.ld_tokens = _rows(res["out"], "out", shape, y.dtype, dev)
-    _call(dev, "taot_combine", ctypes.byref(p), _at(y), _at(perm), _at(counts), _at(weights), _at(residual), _at(res["out"]),
+    _call(dev, "taot_combine", p, _at(y), _at(perm), _at(counts), _at(weights), _at(residual), _at(res["out"]),
           _at(res["info"]))
     return res
 
@@ -339,6 +364,6 @@ def combine_backward(dout: torch.Tensor, perm: torch.Tensor, y: Optional[torch.T
     if len(set(lds)) > 1:
         raise TaotError("y and dy: their rows must be equally far apart")
     p.ld_rows = lds[0]
-    _call(dev, "taot_combine_backward", ctypes.byref(p), _at(dout), _at(y), _at(perm), _at(counts), _at(weights),
+    _call(dev, "taot_combine_backward", p, _at(dout), _at(y), _at(perm), _at(counts), _at(weights),
           _at(res.get("dy")), _at(res.get("dweights")), _at(res["info"]))
     return res

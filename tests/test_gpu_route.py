@@ -69,7 +69,8 @@ def test_route_with_bias(dtype, N, E, k, score):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N,E,k,groups,kept", [(40, 256, 8, 8, 4), (33, 64, 4, 8, 3), (21, 72, 6, 9, 5), (17, 12, 3, 12, 3), (9, 64, 2, 64, 7),
                                                (30, 128, 8, 2, 1), (12, 1024, 8, 32, 4), (25, 160, 6, 8, 3), (19, 256, 8, 4, 2), (7, 512, 8, 8, 4),
-                                               (11, 256, 16, 8, 4), (10, 512, 40, 16, 9), (23, 128, 6, 16, 4), (12, 1024, 8, 64, 3), (8, 40, 2, 20, 2)])
+                                               (14, 536, 8, 8, 2), (9, 98, 6, 2, 1), (16, 268, 8, 4, 3), (9, 40, 16, 4, 4), (6, 6, 2, 2, 1), (8, 656, 8, 4, 4),
+                                               (7, 1000, 16, 8, 3), (10, 72, 6, 8, 5), (11, 256, 16, 8, 4), (10, 512, 40, 16, 9), (23, 128, 6, 16, 4), (12, 1024, 8, 64, 3), (8, 40, 2, 20, 2)])
 @pytest.mark.parametrize("score,with_bias,top", [("sigmoid", True, 2), ("softmax", False, 1), ("sigmoid", False, 2), ("softmax", True, 1)])
 def test_route_by_groups(dtype, N, E, k, groups, kept, score, with_bias, top):
     x = make(N, E, dtype, seed=E + groups)
