@@ -305,7 +305,10 @@ rms_norm_dw_sum_kernel(NormGradArgs a)
 // on their way to shared memory meanwhile, kStages of them (each thread copies, waits for and reads its own columns: no
 // barrier is needed for that); rows that cannot be copied 16 bytes at a time are read when they are due.  A CTA's sums go to the
 // workspace (rms_norm_dw_join_kernel).
-constexpr int kParts = 592;                        // CTAs, four for each of the 148 SMs
+constexpr int kSms = 148;
+constexpr int kSpans = 128;                        // of rows, where a CTA cannot hold a row
+// the most CTAs whose sums a call leaves in the workspace
+int32_t most_parts(int32_t D) { return D <= 2048 ? 4 * kSms : D <= 16384 ? 2 * kSms : kSpans; }
 
 template <typename T, int kLanes, int kRuns>
 struct GradShape {
@@ -517,7 +520,7 @@ cudaError_t fused_as(NormGradArgs& a, cudaStream_t st)
 {
     typedef GradShape<T, kLanes, kRuns> S;
     const size_t ring = WIDE || sizeof(T) == 4 ? S::kRing : 0, sums = a.dweight ? S::kSums : 0, smem = ring > sums ? ring : sums;
-    const int64_t ctas = (a.N + S::kRows - 1) / S::kRows, most = kParts / 4 * (WIDE ? S::kCtasPerSm : S::kCta > kThreads ? 1 : 2);
+    const int64_t ctas = (a.N + S::kRows - 1) / S::kRows, most = kSms * (WIDE ? S::kCtasPerSm : S::kCta > kThreads ? 1 : 2);
     a.parts = (int32_t)(ctas < most ? ctas : most);
     const auto kernel = rms_norm_grad_kernel<T, kLanes, kRuns, WIDE>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -635,7 +638,7 @@ extern "C" int taot_rms_norm_backward_workspace(const taot_norm_params* p, size_
 {
     if (!bytes) return TAOT_ERR_NULL;
     if (const int rc = check(p)) return rc;
-    *bytes = sizeof(float) * (size_t)kParts * p->D;
+    *bytes = sizeof(float) * (size_t)most_parts(p->D) * p->D;
     return TAOT_OK;
 }
 
@@ -658,7 +661,7 @@ extern "C" int taot_rms_norm_backward(const taot_norm_params* p, const void* d_d
     const Range in[] = {range_of(d_dy, N, D, p->ld_y, e), range_of(d_dh, N, D, p->ld_residual, e), range_of(d_h, N, D, p->ld_h, e),
                         range_of(d_weight, 1, D, D, e), range_of(d_rstd, N, 1, 1, 4)};
     const Range out[] = {range_of(d_dx, N, D, p->ld_x, e), range_of(d_dweight, 1, D, D, 4),
-                         range_of(d_dweight ? ws : nullptr, kParts, D, D, 4)};
+                         range_of(d_dweight ? ws : nullptr, most_parts(p->D), D, D, 4)};
     for (int o = 0; o < 3; ++o) {
         for (int i = 0; i < 5; ++i)
             if (overlap(out[o], in[i]) && !(o == 0 && i < 2 && same(out[o], in[i]))) return TAOT_ERR_PARAM;
@@ -669,7 +672,7 @@ extern "C" int taot_rms_norm_backward(const taot_norm_params* p, const void* d_d
     a.dy = d_dy; a.dh = d_dh; a.h = d_h; a.weight = d_weight; a.rstd = d_rstd; a.dx = d_dx;
     a.part = static_cast<float*>(ws); a.dweight = d_dweight;
     a.ld_dy = p->ld_y; a.ld_dh = p->ld_residual; a.ld_h = p->ld_h; a.ld_dx = p->ld_x; a.N = N; a.D = p->D;
-    a.parts = kParts;
+    a.parts = 0;
     a.wide = wide_rows(d_dy, p->ld_y, e) && wide_rows(d_dh, p->ld_residual, e) && wide_rows(d_h, p->ld_h, e) &&
              wide_rows(d_weight, 0, e) && wide_rows(d_dx, p->ld_x, e);
     const unsigned cols = (unsigned)((D + kThreads - 1) / kThreads);
@@ -679,7 +682,7 @@ extern "C" int taot_rms_norm_backward(const taot_norm_params* p, const void* d_d
         TAOT_CUDA_OK(by_type(p->dtype, [&](auto t) { return a.wide ? fused<decltype(t), true>(a, st) : fused<decltype(t), false>(a, st); }));
         return TAOT_OK;
     }
-    a.parts = 128;
+    a.parts = kSpans;
     TAOT_CUDA_OK(by_type(p->dtype, [&](auto t) {
         if (d_dweight) {                                   // before dx, which may take the place of dy
             rms_norm_dw_kernel<decltype(t)><<<dim3(cols, (unsigned)a.parts), kThreads, 0, st>>>(a);

@@ -68,7 +68,7 @@ __device__ __forceinline__ Part part_of(const RowsArgs& a)
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kAll, s, o);
         limit = s < 0 ? 0u : s < (int64_t)a.cap ? (uint32_t)s : a.cap;
     }
-    const bool in0 = (uint32_t)at0 < a.cap, in1 = (uint32_t)at1 < a.cap;
+    const bool in0 = lane >= a.k || (uint32_t)at0 < a.cap, in1 = lane + 32 >= a.k || (uint32_t)at1 < a.cap;
     if (!(in0 && in1) && a.info && p.start == 0) atomicOr(a.info + b, TAOT_INFO_BAD_INDEX);
     // those that are delivered move to the front
     const bool d0 = lane < a.k && in0 && (uint32_t)at0 < limit, d1 = lane + 32 < a.k && in1 && (uint32_t)at1 < limit;

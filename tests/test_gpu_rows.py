@@ -201,6 +201,7 @@ def test_no_entries():
     perm = torch.zeros((2, 3, 0), dtype=torch.int32, device="cuda")
     assert torch.equal(P.combine(y, perm, residual=r)["out"], r) and (P.combine(y, perm)["out"] == 0).all()
     assert P.send(r, perm)["rows"].shape == (2, 0, 16)
+    assert P.combine(y, perm, residual=r)["info"].tolist() == [0, 0]             # no entry, so no bad one
     none = torch.zeros((0, 3, 2), dtype=torch.int32, device="cuda")
     assert P.combine(torch.zeros((0, 6, 16), device="cuda"), none)["out"].shape == (0, 3, 16)
     got = P.combine_backward(torch.zeros((2, 0, 16), device="cuda"), torch.zeros((2, 0, 4), dtype=torch.int32, device="cuda"), y=y)
