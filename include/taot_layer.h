@@ -17,7 +17,8 @@
  * Arrays are aligned to their elements; 16-byte aligned arrays with rows of a multiple of 16 bytes take the wide loads.
  * Sums, norms and scores are held in 32 bits or more and rounded once, at the end.  Same inputs give the same output bits.
  * Errors of every call: TAOT_ERR_NULL, TAOT_ERR_PARAM (struct_size, ranges, an output that overlaps an input or another
- * output where that is not allowed below), TAOT_ERR_UNSUPPORTED, TAOT_ERR_ALIGN, TAOT_ERR_CUDA.
+ * output where that is not allowed below; different columns of one wider array, the same ld apart, do not), TAOT_ERR_UNSUPPORTED,
+ * TAOT_ERR_ALIGN, TAOT_ERR_CUDA.
  */
 #ifndef TAOT_LAYER_H
 #define TAOT_LAYER_H

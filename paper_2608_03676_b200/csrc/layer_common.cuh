@@ -20,15 +20,19 @@ static inline bool misaligned(const void* p, int64_t bytes) { return (reinterpre
 // An array of a call: rows of `cols` elements of `elem` bytes, `ld` elements apart
 struct Range {
     uintptr_t at;
-    int64_t bytes, ld;
+    int64_t bytes, ld, pitch, row;                // from the first element to the last; in bytes: from row to row, of a row
 };
 static inline Range range_of(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t elem)
 {
-    return {reinterpret_cast<uintptr_t>(p), p && rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * elem : 0, ld};
+    return {reinterpret_cast<uintptr_t>(p), p && rows > 0 && cols > 0 ? ((rows - 1) * ld + cols) * elem : 0, ld, ld * elem, cols * elem};
 }
 static inline bool overlap(const Range& a, const Range& b)
 {
-    return a.bytes > 0 && b.bytes > 0 && a.at < b.at + (uintptr_t)b.bytes && b.at < a.at + (uintptr_t)a.bytes;
+    if (a.bytes == 0 || b.bytes == 0 || a.at >= b.at + (uintptr_t)b.bytes || b.at >= a.at + (uintptr_t)a.bytes) return false;
+    if (a.pitch != b.pitch) return true;
+    // rows equally far apart: different columns of one wider array do not meet
+    const uintptr_t pitch = (uintptr_t)a.pitch, off = b.at >= a.at ? (b.at - a.at) % pitch : (pitch - (a.at - b.at) % pitch) % pitch;
+    return off < (uintptr_t)a.row || off + (uintptr_t)b.row > pitch;
 }
 // the same rows at the same place: every element is read before it is written, by the thread that writes it
 static inline bool same(const Range& a, const Range& b) { return a.at == b.at && a.ld == b.ld && a.bytes == b.bytes; }

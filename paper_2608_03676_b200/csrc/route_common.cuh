@@ -417,20 +417,23 @@ __device__ __forceinline__ int gather(const RouteArgs& a, const float* bias, boo
 {
     const int lane = threadIdx.x & 31, size = a.E / a.groups;
     int count = 0;
-#pragma unroll 2
-    for (int e0 = 0; e0 < a.E; e0 += 32) {
-        const int e = e0 + lane, g = min(e, a.E - 1) / size;
-        float v = e < a.E ? logit_at(a.logits, row * a.ld + e, a.dtype) : -INFINITY;
-        if (scored && bias && v > -INFINITY) {
-            const float b = bias[e];
-            v = isfinite(b) ? score_of(a.score, sc, v) + b : -INFINITY;
+    for (int e0 = lane; e0 < a.E + lane; e0 += 256) {              // eight at a time, so that their latencies overlap
+        float v[8], b[8];
+        read_eight(a, row, e0, v);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) b[u] = scored && bias && e0 + 32 * u < a.E ? bias[e0 + 32 * u] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (e0 - lane + 32 * u >= a.E) break;                  // (the same for all lanes)
+            const int e = e0 + 32 * u, g = min(e, a.E - 1) / size;
+            if (scored && bias && v[u] > -INFINITY) v[u] = isfinite(b[u]) ? score_of(a.score, sc, v[u]) + b[u] : -INFINITY;
+            const float limit = __shfl_sync(kAll, least, at + g * step);
+            const bool hit = v[u] > -INFINITY && v[u] >= limit && (kept >> g & 1);
+            const unsigned all = __ballot_sync(kAll, hit);
+            const int place = count + __popc(all & ((1u << lane) - 1));
+            if (hit && place < 32) found[place] = e;
+            count += __popc(all);
         }
-        const float limit = __shfl_sync(kAll, least, at + g * step);
-        const bool hit = v > -INFINITY && v >= limit && (kept >> g & 1);
-        const unsigned all = __ballot_sync(kAll, hit);
-        const int place = count + __popc(all & ((1u << lane) - 1));
-        if (hit && place < 32) found[place] = e;
-        count += __popc(all);
     }
     __syncwarp();
     return count;
@@ -468,9 +471,9 @@ static __device__ __noinline__ bool settle_groups(const RouteArgs& a, int64_t ro
     return true;
 }
 
-// The chosen experts of a row (at most 16, lane j has place j) from those whose key in fp32 is at least `least`, a lower bound of
-// the last chosen one's.  Returns false where there are too many of them.
-static __device__ __noinline__ bool settle_choice(const RouteArgs& a, int64_t row, const Scores sc, uint32_t kept, float least, int32_t* found, int& place)
+// The chosen experts of a row (at most 16; -1 where there is none) go to `found`, from those whose key in fp32 is at least `least`, a lower
+// bound of the last chosen one's.  Returns false where there are too many of them.
+static __device__ __noinline__ bool settle_choice(const RouteArgs& a, int64_t row, const Scores sc, uint32_t kept, float least, int32_t* found)
 {
     const int lane = threadIdx.x & 31;
     const float* bias = a.bias ? a.bias + row / a.T * a.E : nullptr;
@@ -486,9 +489,9 @@ static __device__ __noinline__ bool settle_choice(const RouteArgs& a, int64_t ro
         if (u > mine || (u == mine && f < e)) ++rank;
     }
     __syncwarp();
-    if (lane < count) found[rank] = e;
+    found[lane] = -1;
     __syncwarp();
-    place = lane < min(a.k, count) ? found[lane] : -1;
+    if (lane < count) found[rank] = e;
     __syncwarp();
     return true;
 }

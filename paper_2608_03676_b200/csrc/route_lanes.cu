@@ -439,6 +439,35 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
 #pragma unroll
         for (int h = 0; h < kOwn; ++h) { at[h] = -1; x[h] = -INFINITY; }
     }
+    if (BIAS || GROUP || !kExact) {
+        for (unsigned left = __ballot_sync(kAll, settle || redo); left;) {             // (all lanes are done with the staged rows)
+            const int from = (__ffs(left) - 1) & ~(kLanes - 1);
+            left &= ~(((1u << kLanes) - 1) << from);
+            const int64_t r = first + from / kLanes;
+            const Scores s = {__shfl_sync(kAll, sc.top, from), __shfl_sync(kAll, sc.inv, from)};
+            const float limit = __shfl_sync(kAll, least, from);
+            const uint32_t lanes_kept = __shfl_sync(kAll, kept_lanes, from);
+            uint32_t groups = 1u;
+            if (GROUP) {
+                groups = 0;
+                for (int g = 0; g < a.groups; ++g) groups |= (lanes_kept >> (g << shift) & 1u) << g;
+            }
+            if (__shfl_sync(kAll, (int)redo, from) || !settle_choice(a, r, s, groups, limit, found)) {
+                int at0 = -1, at1 = -1;
+                float t, z;
+                choose_exactly(a, r, reinterpret_cast<uint64_t*>(tile), at0, at1, t, z);
+                found[lane] = at0;
+                __syncwarp();
+            }
+            if ((lane & ~(kLanes - 1)) == from)
+#pragma unroll
+                for (int h = 0; h < kOwn; ++h) {
+                    at[h] = sub + kLanes * h < a.k ? found[sub + kLanes * h] : -1;
+                    x[h] = at[h] >= 0 ? logit_at(a.logits, r * a.ld + at[h], a.dtype) : -INFINITY;
+                }
+            __syncwarp();
+        }
+    }
     float w[kOwn];
     if (a.weights) {
         float most = -INFINITY;
@@ -459,30 +488,10 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
     }
 #pragma unroll
     for (int h = 0; h < kOwn; ++h)
-        if (mine < a.N && !redo && !settle && sub + kLanes * h < a.k) {
+        if (mine < a.N && sub + kLanes * h < a.k) {
             a.topk[row * a.k + sub + kLanes * h] = at[h];
             if (a.weights) a.weights[row * a.k + sub + kLanes * h] = a.scale * w[h];
         }
-    if (BIAS || GROUP || !kExact) {
-        for (unsigned left = __ballot_sync(kAll, settle || redo); left;) {             // (all lanes are done with the rows)
-            const int from = (__ffs(left) - 1) & ~(kLanes - 1);
-            left &= ~(((1u << kLanes) - 1) << from);
-            const int64_t r = first + from / kLanes;
-            const Scores s = {__shfl_sync(kAll, sc.top, from), __shfl_sync(kAll, sc.inv, from)};
-            const float limit = __shfl_sync(kAll, least, from);
-            const uint32_t lanes_kept = __shfl_sync(kAll, kept_lanes, from);
-            uint32_t groups = 1u;
-            if (GROUP) {
-                groups = 0;
-                for (int g = 0, each = kLanes / a.groups; g < a.groups; ++g) groups |= (lanes_kept >> (g * each) & 1u) << g;
-            }
-            int at0 = -1, at1 = -1;
-            float t = s.top, z = __shfl_sync(kAll, total, from);
-            if (__shfl_sync(kAll, (int)redo, from) || !settle_choice(a, r, s, groups, limit, found, at0))
-                choose_exactly(a, r, reinterpret_cast<uint64_t*>(tile), at0, at1, t, z);
-            write_row(a, r, at0, at1, t, z);
-        }
-    }
 }
 
 template <typename T, int K, int U, bool WIDE>

@@ -274,7 +274,9 @@ route_stream_kernel(const __grid_constant__ RouteArgs a, int32_t pitch, int32_t 
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            w[i] = r.at[i] < 0 ? 0.0f : shift ? expf(r.x[i] - r.x[0]) : sigmoid(r.x[i]);
+            w[i] = 0.0f;
+            if (i >= a.k) continue;
+            if (r.at[i] >= 0) w[i] = shift ? expf(r.x[i] - r.x[0]) : sigmoid(r.x[i]);
             sum += w[i];
         }
         if (direct) sum = total;
@@ -313,8 +315,9 @@ route_stream_kernel(const __grid_constant__ RouteArgs a, int32_t pitch, int32_t 
             int at0 = -1, at1 = -1;
             float t = __shfl_sync(kAll, r.x[0], from), z = __shfl_sync(kAll, total, from);
             const float limit = __shfl_sync(kAll, least, from);
-            if (!settle_choice(a, first + from, Scores{t, 1.0f}, 1u, limit, reinterpret_cast<int32_t*>(tile), at0))
-                choose_exactly(a, first + from, reinterpret_cast<uint64_t*>(tile), at0, at1, t, z);
+            int32_t* const found = reinterpret_cast<int32_t*>(tile);
+            if (settle_choice(a, first + from, Scores{t, 1.0f}, 1u, limit, found)) at0 = lane < a.k ? found[lane] : -1;
+            else choose_exactly(a, first + from, reinterpret_cast<uint64_t*>(tile), at0, at1, t, z);
             write_row(a, first + from, at0, at1, t, z);
         }
     }

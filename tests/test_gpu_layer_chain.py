@@ -210,3 +210,27 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(logits[-16:], P.route(wide[-16:].contiguous(), 4)["topk"]) and (logits[0].cpu() == torch.arange(4)).all()
     P.send(y[None].flip(1).contiguous(), perm, out=dict(rows=wide[None]))
     assert torch.equal(wide[-16:], y[-16:])
+
+
+def test_offsets_of_gradients_beyond_32_bits():
+    """The same for the backward passes: the last rows of arrays whose rows are 2^16 elements apart."""
+    import paper_2608_03676_b200 as P
+    Dn, rows, cols = 1 << 16, (1 << 15) + 16, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    a, b = (torch.zeros((rows, Dn), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (a, b):
+        t[:, :cols] = torch.randn((rows, cols), generator=g, device="cuda").bfloat16()
+    x, y = a[:, :cols], b[:, :cols]
+    tail = lambda t: t[-16:].contiguous()
+    w, rstd = torch.ones(cols, dtype=torch.bfloat16, device="cuda"), torch.rand(rows, generator=g, device="cuda")
+    got = P.rms_norm_backward(y, x, w, rstd, dh=y)
+    assert torch.equal(got["dx"][-16:], P.rms_norm_backward(tail(y), tail(x), w, tail(rstd), dh=tail(y))["dx"])
+    topk, dw = P.route(x, 4)["topk"], torch.randn((rows, 4), generator=g, device="cuda")
+    for renormalise in (True, False):
+        want = P.route_backward(tail(x), tail(topk), tail(dw), renormalise=renormalise)
+        assert torch.equal(P.route_backward(x, topk, dw, renormalise=renormalise, out=b[:, 64:128])[-16:], want)
+    perm = torch.arange(rows, dtype=torch.int32, device="cuda").view(1, rows, 1)
+    weights = torch.rand((1, rows, 1), generator=g, device="cuda")
+    got = P.combine_backward(x[None], perm, y=y[None], weights=weights, out=dict(dy=b[None, :, 128:192]))
+    want = P.combine_backward(tail(x)[None], perm[:, :16].contiguous(), y=tail(y)[None], weights=weights[:, -16:].contiguous())
+    assert torch.equal(b[-16:, 128:192], want["dy"][0]) and torch.equal(got["dweights"][0, -16:], want["dweights"][0])

@@ -161,6 +161,10 @@ REFUSED = [
     (combine_grad, dict(dout=None), NULL), (combine_grad, dict(y=None), NULL), (combine_grad, dict(dy=None, dweights=None), NULL), (combine_grad, dict(dy=AT[1]), PARAM),
     (combine_grad, dict(dy=AT[2] + 2), PARAM), (combine_grad, dict(dweights=AT[8]), PARAM), (combine_grad, dict(dweights=AT[5] + 2), ALIGN),
     (combine_grad, dict(dweights=AT[4]), PARAM),
+    # columns of one wider array that meet
+    (combine_grad, dict(dy=AT[2] + 126, ld_rows=128), PARAM), (combine_grad, dict(dy=AT[2] + 130, ld_rows=128), PARAM),
+    (combine_grad, dict(y=AT[2] + 130, dy=AT[2], ld_rows=128), PARAM), (norm, dict(y=AT[1] + 126, ld_x=200, ld_y=200), PARAM),
+    (norm, dict(y=AT[1] + 128, ld_x=200, ld_y=204), PARAM), (route_grad, dict(dlogits=AT[1] + 252, ld_logits=128, ld_dlogits=128), PARAM),
 ]
 
 
@@ -170,7 +174,10 @@ def test_refusals_queue_nothing(so, f, args, want):
     assert not F.log(so)
 
 
-TAKEN = [(norm, dict(residual=AT[5], h=AT[5])), (norm, dict(residual=AT[5], h=AT[1])), (norm, dict(y=AT[1])), (norm, dict(rstd=None)),
+TAKEN = [(combine_grad, dict(dy=AT[2] + 128, ld_rows=128)), (combine_grad, dict(y=AT[2] + 128, dy=AT[2], ld_rows=128)),
+         (norm, dict(y=AT[1] + 128, ld_x=200, ld_y=200)), (norm, dict(x=AT[1] + 400 * 3 + 128, y=AT[1], ld_x=200, ld_y=200)),
+         (route_grad, dict(dlogits=AT[1] + 256, ld_logits=128, ld_dlogits=128)),
+         (norm, dict(residual=AT[5], h=AT[5])), (norm, dict(residual=AT[5], h=AT[1])), (norm, dict(y=AT[1])), (norm, dict(rstd=None)),
          (norm, dict(y=None, q=AT[5], scales=AT[6], group=256)), (norm, dict(dtype=0)), (norm, dict(dtype=2)), (norm_grad, dict(dx=AT[1])),
          (norm_grad, dict(dh=AT[9], dx=AT[9])), (norm_grad, dict(dweight=None, ws=None)), (route, dict(weights=None)), (route, dict(bias=AT[5], mask=AT[6])),
          (route, dict(k=64)), (route, dict(E=1024, ld_logits=1024, k=64)), (route, dict(groups=64, groups_kept=4)), (route_grad, dict(k=64, E=8)),
