@@ -42,7 +42,7 @@ struct Row {
         if (!WIDE) return (r * 8 + i) * kLanes + sub;
         return sizeof(T) == 2 ? (r * kLanes + sub) * 8 + i : r * kLanes * 8 + (i >> 2) * kLanes * 4 + 4 * sub + (i & 3);
     }
-    __device__ __forceinline__ void read(const T* row, int E, int r, float (&x)[8]) const
+    __device__ __forceinline__ Run8<T> read(const T* row, int E, int r) const
     {
         constexpr int kPiece = 16 / (int)sizeof(T);
         Run8<T> v;
@@ -54,7 +54,11 @@ struct Row {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v.v[i] = row[min(expert(r, i), E - 1)];
         }
-        // a NaN and what is closed as the lowest value, an infinity as the largest
+        return v;
+    }
+    // a NaN and what is closed as the lowest value, an infinity as the largest, minus infinity beyond the last expert
+    __device__ __forceinline__ void numbers(const Run8<T>& v, int E, int r, float (&x)[8]) const
+    {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(to_f32(v.v[i]), -Type<T>::big), Type<T>::big);
         if (E != kLanes * 8 * kRuns)
@@ -106,6 +110,11 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
     T* out = static_cast<T*>(a.dlogits) + row * a.ld_out;
     int at[2];
     float g[2], x[2], d[2], base[2] = {0.0f, 0.0f};
+    Run8<T> raw[DENSE ? kRuns : 1];                // (read before the table is waited for)
+    if (DENSE) {
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) raw[r] = cols.read(x_row, a.E, r);
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int j = cols.sub + kLanes * h;
@@ -121,7 +130,7 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
         float e[kRuns][8], top = -INFINITY, total = 0.0f;
 #pragma unroll
         for (int r = 0; r < kRuns; ++r) {
-            cols.read(x_row, a.E, r, e[r]);
+            cols.numbers(raw[r], a.E, r, e[r]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, e[r][i]);
         }
