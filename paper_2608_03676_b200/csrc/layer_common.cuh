@@ -65,12 +65,28 @@ __device__ __forceinline__ void widen(const Run8<T>& r, float (&f)[8])
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = to_f32(r.v[i]);
 }
+// (two at a time: one conversion instruction for both)
+__device__ __forceinline__ uint32_t narrowed_pair(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t narrowed_pair(float a, float b, __half)
+{
+    const __half2 r = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
 template <typename T>
 __device__ __forceinline__ Run8<T> narrowed(const float (&f)[8])
 {
     Run8<T> r;
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(f[i]);
+        for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(&r)[i] = narrowed_pair(f[2 * i], f[2 * i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = f[i];
+    }
     return r;
 }
 

@@ -36,6 +36,27 @@ __device__ __forceinline__ float block_sum(float v, float* part)
     return s;
 }
 
+// The scale of columns whose largest magnitude is `most`, and its reciprocal (to an ulp: it is multiplied before the rounding to 8 bits)
+__device__ __forceinline__ float scale_of(float most) { return max_nan(most * (1.0f / kE4m3Max), kLeastScale); }
+__device__ __forceinline__ float reciprocal(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// four columns in e4m3
+__device__ __forceinline__ uint32_t four_bytes(float a, float b, float c, float d)
+{
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
+           (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
+}
+// 1 / sqrt(v) to 32 bits: the approximation, and a step of Newton's method for a finite one that is not zero
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v);
+    return v > 0.0f && v < INFINITY ? fmaf(r * 0.5f, fmaf(-v * r, r, 1.0f), r) : r;
+}
+
 // the 8-bit form of a lane's eight columns; the lanes of a group of columns share its scale
 __device__ __forceinline__ void write_eight_bit(const NormArgs& a, int64_t row, int c, const float (&y)[8])
 {
@@ -44,13 +65,12 @@ __device__ __forceinline__ void write_eight_bit(const NormArgs& a, int64_t row, 
     for (int i = 0; i < 8; ++i) most = max_nan(most, fabsf(y[i]));
     const int lanes = a.group >> 3;
     for (int o = 1; o < lanes; o <<= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
-    const float scale = max_nan(most / kE4m3Max, kLeastScale);
-    const float inv = 1.0f / scale;
+    const float scale = scale_of(most), by = reciprocal(scale);
     if (c >= a.D) return;
     if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + c / a.group] = scale;
-    union { __nv_fp8_storage_t b[8]; uint2 w; } q;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q.b[i] = __nv_cvt_float_to_fp8(y[i] * inv, __NV_SATFINITE, __NV_E4M3);
+    union { uint8_t b[8]; uint2 w; } q;
+    q.w.x = four_bytes(y[0] * by, y[1] * by, y[2] * by, y[3] * by);
+    q.w.y = four_bytes(y[4] * by, y[5] * by, y[6] * by, y[7] * by);
     uint8_t* to = a.q + row * a.ld_q + c;
     if (a.wide && c + 8 <= a.D) *reinterpret_cast<uint2*>(to) = q.w;
     else
@@ -85,7 +105,7 @@ rms_norm_kernel(NormArgs a)
         for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
     }
     // (divided by D before the sums of the threads are added: those squares may add up to more than the mean may be)
-    const float rstd = 1.0f / sqrtf(block_sum<kThreads / 32>(sum * (1.0f / (float)a.D), part) + a.eps);
+    const float rstd = inverse_root(block_sum<kThreads / 32>(sum * (1.0f / (float)a.D), part) + a.eps);
     if (tid == 0 && a.rstd) a.rstd[row] = rstd;
     const T* from = res ? h : x;
     const int end = (a.D + 255) / 256 * 256;              // whole warps: the lanes of a group stay together
@@ -162,7 +182,7 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
         sum = sum_of_warps<kWarpsOfRow>(part + slot * kWarpsOfRow);
     }
     if (!there) return;                            // (whole warps)
-    const float rstd = 1.0f / sqrtf(sum + a.eps);
+    const float rstd = inverse_root(sum + a.eps);
     if (a.rstd && tid % kLanes == 0) a.rstd[row] = rstd;
 #pragma unroll
     for (int r = 0; r < kRuns; ++r) {
@@ -189,12 +209,10 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int c = column<WIDE, T>(c0, lane, 4 * q);
-                const float scale = max_nan(most[q] / kE4m3Max, kLeastScale), by = 1.0f / scale;
+                const float scale = scale_of(most[q]), by = reciprocal(scale);
                 if (c >= a.D) continue;
                 if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + c / a.group] = scale;
-                uint32_t word = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) word |= (uint32_t)__nv_cvt_float_to_fp8(f[4 * q + i] * by, __NV_SATFINITE, __NV_E4M3) << (8 * i);
+                const uint32_t word = four_bytes(f[4 * q] * by, f[4 * q + 1] * by, f[4 * q + 2] * by, f[4 * q + 3] * by);
                 *reinterpret_cast<uint32_t*>(a.q + row * a.ld_q + c) = word;
             }
         } else {
@@ -216,10 +234,10 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
             for (int i = 0; i < 8; ++i) {
 #pragma unroll
                 for (int o = 16; o; o >>= 1) most[i] = max_nan(most[i], __shfl_xor_sync(0xffffffffu, most[i], o));
-                const float scale = max_nan(most[i] / kE4m3Max, kLeastScale);
+                const float scale = scale_of(most[i]);
                 const int c = c0 + 32 * i + lane;
                 if (lane == 0 && (i & (n - 1)) == 0 && c < a.D) a.scales[row * a.scale_cols + c / a.group] = scale;
-                if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(f[i] * (1.0f / scale), __NV_SATFINITE, __NV_E4M3);
+                if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(f[i] * reciprocal(scale), __NV_SATFINITE, __NV_E4M3);
             }
         }
     }
