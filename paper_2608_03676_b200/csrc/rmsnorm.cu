@@ -20,7 +20,7 @@ struct NormArgs {
     float *scales, *rstd;
     int64_t ld_x, ld_residual, ld_h, ld_y, ld_q;
     int64_t N;
-    int32_t D, group, scale_cols, wide;
+    int32_t D, group, group_shift, scale_cols, wide;
     float eps;
 };
 
@@ -67,7 +67,7 @@ __device__ __forceinline__ void write_eight_bit(const NormArgs& a, int64_t row, 
     for (int o = 1; o < lanes; o <<= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
     const float scale = scale_of(most), by = reciprocal(scale);
     if (c >= a.D) return;
-    if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + c / a.group] = scale;
+    if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
     union { uint8_t b[8]; uint2 w; } q;
     q.w.x = four_bytes(y[0] * by, y[1] * by, y[2] * by, y[3] * by);
     q.w.y = four_bytes(y[4] * by, y[5] * by, y[6] * by, y[7] * by);
@@ -211,7 +211,7 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
                 const int c = column<WIDE, T>(c0, lane, 4 * q);
                 const float scale = scale_of(most[q]), by = reciprocal(scale);
                 if (c >= a.D) continue;
-                if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + c / a.group] = scale;
+                if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
                 const uint32_t word = four_bytes(f[4 * q] * by, f[4 * q + 1] * by, f[4 * q + 2] * by, f[4 * q + 3] * by);
                 *reinterpret_cast<uint32_t*>(a.q + row * a.ld_q + c) = word;
             }
@@ -236,7 +236,7 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
                 for (int o = 16; o; o >>= 1) most[i] = max_nan(most[i], __shfl_xor_sync(0xffffffffu, most[i], o));
                 const float scale = scale_of(most[i]);
                 const int c = c0 + 32 * i + lane;
-                if (lane == 0 && (i & (n - 1)) == 0 && c < a.D) a.scales[row * a.scale_cols + c / a.group] = scale;
+                if (lane == 0 && (i & (n - 1)) == 0 && c < a.D) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
                 if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(f[i] * reciprocal(scale), __NV_SATFINITE, __NV_E4M3);
             }
         }
@@ -635,6 +635,7 @@ extern "C" int taot_rms_norm(const taot_norm_params* p, const void* d_x, const v
     NormArgs a;
     a.x = d_x; a.residual = d_residual; a.weight = d_weight; a.h = d_h; a.y = d_y; a.q = d_q; a.scales = d_scales; a.rstd = d_rstd;
     a.ld_x = p->ld_x; a.ld_residual = p->ld_residual; a.ld_h = p->ld_h; a.ld_y = p->ld_y; a.ld_q = p->ld_q;
+    a.group_shift = p->group == 32 ? 5 : p->group == 64 ? 6 : p->group == 128 ? 7 : 8;
     a.N = N; a.D = p->D; a.group = p->group; a.scale_cols = (int32_t)cols; a.eps = p->eps;
     a.wide = wide_rows(d_x, p->ld_x, e) && wide_rows(d_residual, p->ld_residual, e) && wide_rows(d_weight, 0, e) &&
              wide_rows(d_h, p->ld_h, e) && wide_rows(d_y, p->ld_y, e) && !misaligned(d_q, 8) && (!d_q || p->ld_q % 8 == 0);

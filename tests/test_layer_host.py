@@ -207,3 +207,56 @@ def test_the_workspace_is_asked_for(so):
     assert so.taot_rms_norm_backward_workspace(ctypes.byref(norm_params(D=0)), ctypes.byref(n)) == PARAM
     assert so.taot_rms_norm_backward_workspace(ctypes.byref(norm_params()), None) == NULL
     assert so.taot_rms_norm_backward_workspace(None, ctypes.byref(n)) == NULL
+
+
+def test_a_call_makes_its_tensors_device_current_and_takes_that_devices_stream(monkeypatch):
+    import torch
+    from paper_2608_03676_b200 import layer
+    current, log = [0], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = device.index
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.index
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    def entry(params, *args):
+        log.append((current[0], args))
+        return 0
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(layer, "_stream_of", lambda index: 1000 + index)
+    monkeypatch.setitem(layer._functions, "taot_route", entry)
+    for index in (0, 1, 0):
+        layer._call(torch.device("cuda", index), "taot_route", RouteParams(), 7)
+    assert log == [(0, (7, 1000)), (1, (7, 1001)), (0, (7, 1000))] and current == [0]
+    monkeypatch.setitem(layer._functions, "taot_route", lambda *a: PARAM)
+    with pytest.raises(layer.TaotError, match="out of range"):
+        layer._call(torch.device("cuda", 1), "taot_route", RouteParams(), 7)
+    assert current == [0]
+
+
+def test_which_strides_are_rows():
+    import torch
+    from paper_2608_03676_b200 import layer
+    cpu = torch.device("cpu")
+    rows = lambda t: layer._rows(t, "t", t.shape, t.dtype, cpu)
+    x = torch.zeros((2, 3, 4, 10))
+    assert rows(x) == 10 and rows(x[..., 2:7]) == 10 and rows(x[:, :, ::2, :5]) == 20 and rows(x[1:, 2:, 3:, 1:4]) == 3
+    assert rows(x[0, 0, :, :1]) == 10 and rows(x[0, 0, 0, 3:5]) == 2 and rows(torch.zeros((0, 5))) == 5 and rows(torch.zeros((4, 1)).expand(4, 1)) == 1
+    for bad in (x.transpose(2, 3), x[..., ::2], x[:, :2], x[:, :, :3], torch.zeros((1, 6)).expand(4, 6), torch.zeros(6).as_strided((3, 4), (1, 1)),
+                x.transpose(0, 1)):
+        with pytest.raises(layer.TaotError):
+            rows(bad)
+    with pytest.raises(layer.TaotError, match="expected a tensor"):
+        layer._rows(x, "t", (2, 3, 4, 9), x.dtype, cpu)
+    with pytest.raises(layer.TaotError, match="expected a tensor"):
+        layer._rows(x, "t", x.shape, torch.bfloat16, cpu)
+    with pytest.raises(layer.TaotError):
+        layer._dense(x[..., :5], "t", (2, 3, 4, 5), x.dtype, cpu)
+    layer._dense(None, "t", (1,), x.dtype, cpu)
