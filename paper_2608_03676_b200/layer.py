@@ -42,6 +42,7 @@ class RowsParams(ctypes.Structure):
                 ("ld_rows", ctypes.c_int64), ("ld_tokens", ctypes.c_int64), ("ld_residual", ctypes.c_int64)]
 
 
+_NORM_BYTES, _ROUTE_BYTES, _ROWS_BYTES = (ctypes.sizeof(t) for t in (NormParams, RouteParams, RowsParams))
 _P, _I = ctypes.c_void_p, ctypes.c_int32
 _ARGS = {                                        # behind the pointer to the params; the stream comes last
     "taot_rms_norm": [_P] * 8, "taot_rms_norm_backward": [_P] * 8, "taot_route": [_P] * 5, "taot_route_backward": [_P] * 4,
@@ -133,9 +134,21 @@ def _count(shape) -> int:
     return n
 
 
-def _slot(out: Optional[Dict[str, torch.Tensor]], name: str, shape, dtype, device) -> torch.Tensor:
+def _take(out: Optional[Dict[str, torch.Tensor]], name: str, shape, dtype, device):
+    """An output whose last dimension is a row, and the distance between rows: the caller's, checked, or a new one."""
     t = None if out is None else out.get(name)
-    return torch.empty(shape, dtype=dtype, device=device) if t is None else t
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device), shape[-1]
+    return t, _rows(t, name, shape, dtype, device)
+
+
+def _take_dense(out: Optional[Dict[str, torch.Tensor]], name: str, shape, dtype, device) -> torch.Tensor:
+    """A contiguous output: the caller's, checked, or a new one."""
+    t = None if out is None else out.get(name)
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _dense(t, name, shape, dtype, device)
+    return t
 
 
 # ---------------------------------------------------------------------------------------------------------------------
@@ -156,25 +169,24 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
         raise TaotError("rms_norm: nothing to write (want_y is False and group is 0)")
     code = _type(x, "x")
     _dense(weight, "weight", (D,), x.dtype, dev)
-    p = NormParams(ctypes.sizeof(NormParams), code, _count(lead), D, group, eps, 0)
-    p.ld_x = _rows(x, "x", x.shape, x.dtype, dev)
-    res = dict(rstd=_slot(out, "rstd", lead, torch.float32, dev))
-    _dense(res["rstd"], "rstd", lead, torch.float32, dev)
+    shape, dtype = x.shape, x.dtype
+    rstd = _take_dense(out, "rstd", lead, torch.float32, dev)
+    h = y = q = scales = None
+    ld_x, ld_res, ld_h, ld_y, ld_q = _rows(x, "x", shape, dtype, dev), 0, 0, 0, 0
+    res = dict(rstd=rstd)
     if residual is not None:
-        p.ld_residual = _rows(residual, "residual", x.shape, x.dtype, dev)
-        res["h"] = _slot(out, "h", x.shape, x.dtype, dev)
-        p.ld_h = _rows(res["h"], "h", x.shape, x.dtype, dev)
+        ld_res = _rows(residual, "residual", shape, dtype, dev)
+        h, ld_h = _take(out, "h", shape, dtype, dev)
+        res["h"] = h
     if want_y:
-        res["y"] = _slot(out, "y", x.shape, x.dtype, dev)
-        p.ld_y = _rows(res["y"], "y", x.shape, x.dtype, dev)
+        y, ld_y = _take(out, "y", shape, dtype, dev)
+        res["y"] = y
     if group:
-        cols = lead + (-(-D // group) if group > 0 else 0,)
-        res["q"] = _slot(out, "q", x.shape, torch.float8_e4m3fn, dev)
-        res["scales"] = _slot(out, "scales", cols, torch.float32, dev)
-        p.ld_q = _rows(res["q"], "q", x.shape, torch.float8_e4m3fn, dev)
-        _dense(res["scales"], "scales", cols, torch.float32, dev)
-    _call(dev, "taot_rms_norm", p, _at(x), _at(residual), _at(weight), _at(res.get("h")), _at(res.get("y")),
-          _at(res.get("q")), _at(res.get("scales")), _at(res["rstd"]))
+        q, ld_q = _take(out, "q", shape, torch.float8_e4m3fn, dev)
+        scales = _take_dense(out, "scales", lead + (-(-D // group) if group > 0 else 0,), torch.float32, dev)
+        res["q"], res["scales"] = q, scales
+    p = NormParams(_NORM_BYTES, code, _count(lead), D, group, eps, 0, ld_x, ld_res, ld_h, ld_y, ld_q)
+    _call(dev, "taot_rms_norm", p, _at(x), _at(residual), _at(weight), _at(h), _at(y), _at(q), _at(scales), _at(rstd))
     return res
 
 
@@ -189,21 +201,20 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
     code = _type(h, "h")
     _dense(weight, "weight", (D,), h.dtype, dev)
     _dense(rstd, "rstd", lead, torch.float32, dev)
-    p = NormParams(ctypes.sizeof(NormParams), code, _count(lead), D, 0, 0.0, 0)
+    p = NormParams(_NORM_BYTES, code, _count(lead), D, 0, 0.0, 0)
     p.ld_h = _rows(h, "h", h.shape, h.dtype, dev)
     p.ld_y = _rows(dy, "dy", h.shape, h.dtype, dev)
     if dh is not None:
         p.ld_residual = _rows(dh, "dh", h.shape, h.dtype, dev)
-    res = dict(dx=_slot(out, "dx", h.shape, h.dtype, dev))
-    p.ld_x = _rows(res["dx"], "dx", h.shape, h.dtype, dev)
+    dx, p.ld_x = _take(out, "dx", h.shape, h.dtype, dev)
+    res = dict(dx=dx)
     ws = None
     if want_dweight:
-        res["dweight"] = _slot(out, "dweight", (D,), torch.float32, dev)
-        _dense(res["dweight"], "dweight", (D,), torch.float32, dev)
+        res["dweight"] = _take_dense(out, "dweight", (D,), torch.float32, dev)
         n = ctypes.c_size_t()
         _check(load_library().taot_rms_norm_backward_workspace(ctypes.byref(p), ctypes.byref(n)), "taot_rms_norm_backward_workspace")
         ws = torch.empty(n.value, dtype=torch.uint8, device=dev)     # of this call alone: its stream's allocator takes it back
-    _call(dev, "taot_rms_norm_backward", p, _at(dy), _at(dh), _at(h), _at(weight), _at(rstd), _at(res["dx"]),
+    _call(dev, "taot_rms_norm_backward", p, _at(dy), _at(dh), _at(h), _at(weight), _at(rstd), _at(dx),
           _at(res.get("dweight")), _at(ws))
     return res
 
@@ -219,7 +230,7 @@ def _route_params(logits: torch.Tensor, k: int, score: str, renormalise: bool, s
     lead = logits.shape[:-1]
     T = lead[-1]
     L = _count(lead[:-1])
-    p = RouteParams(ctypes.sizeof(RouteParams), code, L, T, logits.shape[-1], k, _SCORES[score], 1, 1, 1, int(bool(renormalise)), scale)
+    p = RouteParams(_ROUTE_BYTES, code, L, T, logits.shape[-1], k, _SCORES[score], 1, 1, 1, int(bool(renormalise)), scale)
     p.ld_logits = _rows(logits, "logits", logits.shape, logits.dtype, logits.device)
     return p, lead
 
@@ -241,11 +252,9 @@ def route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optional[t
             raise TaotError(f"bias: expected [{p.E}] or [{p.L}, {p.E}], not {list(bias.shape)}")
     _dense(mask, "mask", lead, torch.bool, dev)
     shape = lead + (k,)
-    res = dict(topk=_slot(out, "topk", shape, torch.int32, dev))
-    _dense(res["topk"], "topk", shape, torch.int32, dev)
+    res = dict(topk=_take_dense(out, "topk", shape, torch.int32, dev))
     if want_weights:
-        res["weights"] = _slot(out, "weights", shape, torch.float32, dev)
-        _dense(res["weights"], "weights", shape, torch.float32, dev)
+        res["weights"] = _take_dense(out, "weights", shape, torch.float32, dev)
     _call(dev, "taot_route", p, _at(logits), _at(bias), _at(mask), _at(res["topk"]), _at(res.get("weights")))
     return res
 
@@ -271,9 +280,10 @@ def route_backward(logits: torch.Tensor, topk: torch.Tensor, dweights: torch.Ten
 
 def _rows_params(perm: torch.Tensor, counts: Optional[torch.Tensor], D: int, code: int):
     dev = _start(perm, "perm", 2)
-    lead, n, k = tuple(perm.shape[:-2]), perm.shape[-2], perm.shape[-1]
+    shape = perm.shape
+    lead, n, k = shape[:-2], shape[-2], shape[-1]
     _dense(perm, "perm", perm.shape, torch.int32, dev)
-    p = RowsParams(ctypes.sizeof(RowsParams), code, _count(lead), n, k, D, 0, 0)
+    p = RowsParams(_ROWS_BYTES, code, _count(lead), n, k, D, 0, 0)
     if counts is not None:
         if counts.dim() != len(lead) + 1 or counts.shape[-1] < 1:
             raise TaotError(f"counts: expected {list(lead)} + [C]")
@@ -305,16 +315,15 @@ def send(x: torch.Tensor, perm: torch.Tensor, counts: Optional[torch.Tensor] = N
     p.ld_tokens = _rows(x, "x", shape, x.dtype, dev)
     if x.element_size() not in (1, 2, 4):
         raise TaotError(f"x: expected elements of 1, 2 or 4 bytes, not {x.dtype}")
-    res = dict(rows=_slot(out, "rows", lead + (n * k, D), x.dtype, dev), info=_info(out, lead, dev))
-    p.ld_rows = _rows(res["rows"], "rows", lead + (n * k, D), x.dtype, dev)
+    rows, p.ld_rows = _take(out, "rows", lead + (n * k, D), x.dtype, dev)
+    res = dict(rows=rows, info=_info(out, lead, dev))
     cols = 0
     if scales is not None:
         if scales.dim() < 1:
             raise TaotError("scales: expected [.., n, G]")
         cols = scales.shape[-1]
         _dense(scales, "scales", lead + (n, cols), torch.float32, dev)
-        res["scales"] = _slot(out, "scales", lead + (n * k, cols), torch.float32, dev)
-        _dense(res["scales"], "scales", lead + (n * k, cols), torch.float32, dev)
+        res["scales"] = _take_dense(out, "scales", lead + (n * k, cols), torch.float32, dev)
     _call(dev, "taot_send", p, x.element_size(), _at(x), _at(scales), cols, _at(perm),
           _at(counts), _at(res["rows"]), _at(res.get("scales")), _at(res["info"]))
     return res
@@ -332,8 +341,8 @@ def combine(y: torch.Tensor, perm: torch.Tensor, weights: Optional[torch.Tensor]
     shape = lead + (n, D)
     if residual is not None:
         p.ld_residual = _rows(residual, "residual", shape, y.dtype, dev)
-    res = dict(out=_slot(out, "out", shape, y.dtype, dev), info=_info(out, lead, dev))
-    p.ld_tokens = _rows(res["out"], "out", shape, y.dtype, dev)
+    into, p.ld_tokens = _take(out, "out", shape, y.dtype, dev)
+    res = dict(out=into, info=_info(out, lead, dev))
     _call(dev, "taot_combine", p, _at(y), _at(perm), _at(counts), _at(weights), _at(residual), _at(res["out"]),
           _at(res["info"]))
     return res
@@ -356,11 +365,10 @@ def combine_backward(dout: torch.Tensor, perm: torch.Tensor, y: Optional[torch.T
     lds = []
     if y is not None:
         lds.append(_rows(y, "y", rows, dout.dtype, dev))
-        res["dweights"] = _slot(out, "dweights", tuple(perm.shape), torch.float32, dev)
-        _dense(res["dweights"], "dweights", perm.shape, torch.float32, dev)
+        res["dweights"] = _take_dense(out, "dweights", perm.shape, torch.float32, dev)
     if want_dy:
-        res["dy"] = _slot(out, "dy", rows, dout.dtype, dev)
-        lds.append(_rows(res["dy"], "dy", rows, dout.dtype, dev))
+        res["dy"], ld = _take(out, "dy", rows, dout.dtype, dev)
+        lds.append(ld)
     if len(set(lds)) > 1:
         raise TaotError("y and dy: their rows must be equally far apart")
     p.ld_rows = lds[0]
