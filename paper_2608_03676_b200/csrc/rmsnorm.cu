@@ -230,14 +230,19 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) most[i] = max_nan(most[i], other[i]);
                 }
+            float by = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                for (int o = 16; o; o >>= 1) most[i] = max_nan(most[i], __shfl_xor_sync(0xffffffffu, most[i], o));
-                const float scale = scale_of(most[i]);
                 const int c = c0 + 32 * i + lane;
-                if (lane == 0 && (i & (n - 1)) == 0 && c < a.D) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
-                if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(f[i] * reciprocal(scale), __NV_SATFINITE, __NV_E4M3);
+                if ((i & (n - 1)) == 0) {          // the first of a group (the same for a warp)
+                    float m = most[i];
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    const float scale = scale_of(m);
+                    by = reciprocal(scale);
+                    if (lane == 0 && c < a.D) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
+                }
+                if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(f[i] * by, __NV_SATFINITE, __NV_E4M3);
             }
         }
     }
