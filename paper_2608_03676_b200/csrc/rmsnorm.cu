@@ -132,7 +132,7 @@ __device__ __forceinline__ float sum_of_warps(const float* part)
 
 // Rows of up to 8192 columns: `kLanes` threads hold a row, `kRuns` runs of eight columns each, from the addition to the 8-bit form.
 template <typename T, int kLanes, int kRuns, bool WIDE>
-__global__ void __launch_bounds__(kLanes > kThreads ? kLanes : kThreads, WIDE && sizeof(T) == 2 && kLanes <= kThreads ? (kRuns == 1 ? 6 : 5) : 1)
+__global__ void __launch_bounds__(kLanes > kThreads ? kLanes : kThreads, !WIDE ? (kLanes > kThreads ? 2 : 4) : sizeof(T) == 2 && kLanes <= kThreads ? (kRuns == 1 ? 6 : 5) : 1)
 rms_norm_row_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int kCta = kLanes > kThreads ? kLanes : kThreads;
