@@ -36,14 +36,79 @@ __device__ __forceinline__ float block_sum(float v, float* part)
     return s;
 }
 
-// The scale of columns whose largest magnitude is `most`, and its reciprocal (to an ulp: it is multiplied before the rounding to 8 bits)
-__device__ __forceinline__ float scale_of(float most) { return max_nan(most * (1.0f / kE4m3Max), kLeastScale); }
-__device__ __forceinline__ float reciprocal(float v)
+// two products (and sums) in an instruction, each rounded as by itself
+__device__ __forceinline__ uint64_t two(float a, float b)
 {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ void apart(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t times(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t times_plus(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// eight columns times rstd, times their weights
+__device__ __forceinline__ void normalise(float (&f)[8], float rstd, const float (&w)[8])
+{
+    const uint64_t r = two(rstd, rstd);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) apart(times(times(two(f[i], f[i + 1]), r), two(w[i], w[i + 1])), f[i], f[i + 1]);
+}
+
+// The scale of columns whose largest magnitude is `most`, and the columns divided by it.  The 8-bit values are those of the fp32
+// quotients to the bit: quotients in the middle of two 8-bit values are frequent (16-bit inputs, weights of one), and a product
+// with the reciprocal takes the other one there (8192 x 4096 bf16: 56.8 us with the product, 60.0 with the quotient).
+//   a / b: with b's reciprocal in two parts (`by` rounded to nearest, and what it lacks, `low`) the product q = a by + a low is
+//   within an ulp, and Markstein's step (1990), q + (a - q b) by, whose remainder is exact, is the quotient rounded to nearest, as
+//   long as no remainder comes below 2^-149: columns below 2^-60 and their scale are taken times 2^100.  There is no branch: an infinite
+//   scale has the reciprocal 0 (0 for finite columns, a NaN for infinite ones), a NaN spreads.
+struct Scale {
+    float value, up, b, by, low;                   // b = value * up
+    __device__ __forceinline__ explicit Scale(float most)
+    {
+        constexpr float inv = 1.0f / kE4m3Max, rest = (float)(1.0 / (double)kE4m3Max - (double)inv);
+        const bool small = most < 0x1p-60f;
+        up = small ? 0x1p100f : 1.0f;
+        const float m = most * up, q = fmaf(m, inv, m * rest);
+        value = fmaxf(fmaf(fmaf(-q, kE4m3Max, m), inv, q) * (small ? 0x1p-100f : 1.0f), kLeastScale);
+        value = most < INFINITY ? value : most;
+        b = value * up;
+        // the approximation is within an ulp; a step of Newton's method rounds it to nearest, except where all bits of the mantissa are
+        // set (Markstein): there the nearest one's last bit is set too
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(by) : "f"(b));
+        by = fmaf(by, fmaf(-by, b, 1.0f), by);
+        if ((__float_as_uint(b) & 0x7fffffu) == 0x7fffffu) by = __uint_as_float(__float_as_uint(by) | 1u);
+        low = fmaf(-by, b, 1.0f) * by;
+        if (value == INFINITY) { b = 1.0f; by = low = 0.0f; }
+    }
+    __device__ __forceinline__ float divide(float f) const
+    {
+        const float a = f * up, q = fmaf(a, by, a * low);
+        return copysignf(fmaf(fmaf(-q, b, a), by, q), f);          // (zeros have signs)
+    }
+    template <int n>
+    __device__ __forceinline__ void divide(const float* f, float (&out)[n]) const      // the same, two at a time
+    {
+        static_assert(n % 2 == 0, "two at a time");
+        const uint64_t ups = two(up, up), minus = two(-b, -b), bys = two(by, by), lows = two(low, low);
+#pragma unroll
+        for (int i = 0; i < n; i += 2) {
+            const uint64_t a = times(two(f[i], f[i + 1]), ups), q = times_plus(a, bys, times(a, lows));
+            apart(times_plus(times_plus(q, minus, a), bys, q), out[i], out[i + 1]);
+            out[i] = copysignf(out[i], f[i]);
+            out[i + 1] = copysignf(out[i + 1], f[i + 1]);
+        }
+    }
+};
 // four columns in e4m3
 __device__ __forceinline__ uint32_t four_bytes(float a, float b, float c, float d)
 {
@@ -63,14 +128,18 @@ __device__ __forceinline__ void write_eight_bit(const NormArgs& a, int64_t row, 
     float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = max_nan(most, fabsf(y[i]));
-    const int lanes = a.group >> 3;
-    for (int o = 1; o < lanes; o <<= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
-    const float scale = scale_of(most), by = reciprocal(scale);
+    if (c >= a.D) most = 0.0f;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2)
+        if (o < 4 || a.group > 8 * o) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
     if (c >= a.D) return;
-    if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
+    const Scale scale(most);
+    if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale.value;
+    float v[8];
+    scale.divide(y, v);
     union { uint8_t b[8]; uint2 w; } q;
-    q.w.x = four_bytes(y[0] * by, y[1] * by, y[2] * by, y[3] * by);
-    q.w.y = four_bytes(y[4] * by, y[5] * by, y[6] * by, y[7] * by);
+    q.w.x = four_bytes(v[0], v[1], v[2], v[3]);
+    q.w.y = four_bytes(v[4], v[5], v[6], v[7]);
     uint8_t* to = a.q + row * a.ld_q + c;
     if (a.wide && c + 8 <= a.D) *reinterpret_cast<uint2*>(to) = q.w;
     else
@@ -141,7 +210,9 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
     const int tid = threadIdx.x, lane = tid & 31, slot = tid / kLanes, start = (tid % kLanes >> 5) * 256;
     const int64_t row = (int64_t)blockIdx.x * (kCta / kLanes) + slot;
     const bool there = row < a.N;
-    const auto live = [&](int r, int i) { return there && column<WIDE, T>(start + r * kLanes * 8, lane, i) < a.D; };
+    // (pieces of 16 bytes are within the row or beyond it as a whole)
+    constexpr int kPiece = WIDE ? 16 / (int)sizeof(T) : 1;
+    const auto live = [&](int r, int i) { return column<WIDE, T>(start + r * kLanes * 8, lane, i / kPiece * kPiece) < a.D; };
     Run8<T> h[kRuns], w[kRuns];
     float sum = 0.0f;
     if (there) {
@@ -190,8 +261,7 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
         float f[8], g[8];
         widen(h[r], f);
         widen(w[r], g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = live(r, i) ? f[i] * rstd * g[i] : 0.0f;
+        normalise(f, rstd, g);                     // (what is beyond D is not written)
         if (a.y) store8<WIDE>(static_cast<T*>(a.y) + row * a.ld_y, c0, lane, a.D, narrowed<T>(f));
         if (!a.q || c0 >= a.D) continue;           // (the same for a warp)
         if (WIDE && sizeof(T) == 2) {
@@ -200,7 +270,10 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
             // columns 4 lane to 4 lane + 3 of either half of the warp's 256
             float most[2];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) most[q] = max_nan(max_nan(fabsf(f[4 * q]), fabsf(f[4 * q + 1])), max_nan(fabsf(f[4 * q + 2]), fabsf(f[4 * q + 3])));
+            for (int q = 0; q < 2; ++q) {
+                most[q] = max_nan(max_nan(fabsf(f[4 * q]), fabsf(f[4 * q + 1])), max_nan(fabsf(f[4 * q + 2]), fabsf(f[4 * q + 3])));
+                if (!live(r, 4 * q)) most[q] = 0.0f;
+            }
             if (a.group == 256) most[0] = most[1] = max_nan(most[0], most[1]);
             for (int o = 1; o < min(a.group >> 2, 32); o <<= 1) {
                 most[0] = max_nan(most[0], __shfl_xor_sync(0xffffffffu, most[0], o));
@@ -209,17 +282,19 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 const int c = column<WIDE, T>(c0, lane, 4 * q);
-                const float scale = scale_of(most[q]), by = reciprocal(scale);
                 if (c >= a.D) continue;
-                if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
-                const uint32_t word = four_bytes(f[4 * q] * by, f[4 * q + 1] * by, f[4 * q + 2] * by, f[4 * q + 3] * by);
+                const Scale scale(most[q]);
+                if ((c & (a.group - 1)) == 0) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale.value;
+                float v[4];
+                scale.divide(f + 4 * q, v);
+                const uint32_t word = four_bytes(v[0], v[1], v[2], v[3]);
                 *reinterpret_cast<uint32_t*>(a.q + row * a.ld_q + c) = word;
             }
         } else {
             // column 32 i + lane of the warp's 256: a group is 1, 2, 4 or 8 of the i
             float most[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) most[i] = fabsf(f[i]);
+            for (int i = 0; i < 8; ++i) most[i] = live(r, i) ? fabsf(f[i]) : 0.0f;
             const int n = a.group >> 5;
 #pragma unroll
             for (int o = 1; o < 8; o *= 2)
@@ -230,7 +305,7 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) most[i] = max_nan(most[i], other[i]);
                 }
-            float by = 0.0f;
+            Scale scale(0.0f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int c = c0 + 32 * i + lane;
@@ -238,11 +313,10 @@ rms_norm_row_kernel(const __grid_constant__ NormArgs a)
                     float m = most[i];
 #pragma unroll
                     for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    const float scale = scale_of(m);
-                    by = reciprocal(scale);
-                    if (lane == 0 && c < a.D) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale;
+                    scale = Scale(m);
+                    if (lane == 0 && c < a.D) a.scales[row * a.scale_cols + (c >> a.group_shift)] = scale.value;
                 }
-                if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(f[i] * by, __NV_SATFINITE, __NV_E4M3);
+                if (c < a.D) a.q[row * a.ld_q + c] = __nv_cvt_float_to_fp8(scale.divide(f[i]), __NV_SATFINITE, __NV_E4M3);
             }
         }
     }
