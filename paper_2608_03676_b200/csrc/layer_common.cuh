@@ -43,6 +43,16 @@ static inline bool wide_rows(const void* p, int64_t ld, int64_t elem)
     return !p || (!misaligned(p, 16) && ld * elem % 16 == 0);
 }
 
+// Lets a kernel have up to `most` bytes of dynamic shared memory.  The limit belongs to the kernel, in all of the context: a call that
+// set its own could lower it between another host thread's setting and launch.  So `most` is the most that any call's launch of
+// the kernel takes, whatever the call at hand needs.
+constexpr size_t kWithoutLimit = 46 * 1024;        // 48 KB less what these kernels declare
+template <typename K>
+cudaError_t allow_shared(K kernel, size_t most)
+{
+    return most <= kWithoutLimit ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
+
 #ifdef __CUDACC__
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }

@@ -616,11 +616,12 @@ template <typename T, bool WIDE, int kLanes, int kRuns>
 cudaError_t fused_as(NormGradArgs& a, cudaStream_t st)
 {
     typedef GradShape<T, kLanes, kRuns> S;
-    const size_t ring = WIDE || sizeof(T) == 4 ? S::kRing : 0, sums = a.dweight ? S::kSums : 0, smem = ring > sums ? ring : sums;
+    constexpr size_t ring = WIDE || sizeof(T) == 4 ? S::kRing : 0, most_smem = ring > S::kSums ? ring : S::kSums;
+    const size_t sums = a.dweight ? S::kSums : 0, smem = ring > sums ? ring : sums;
     const int64_t ctas = (a.N + S::kRows - 1) / S::kRows, most = kSms * (WIDE ? S::kCtasPerSm : S::kCta > kThreads ? 1 : 2);
     a.parts = (int32_t)(ctas < most ? ctas : most);
     const auto kernel = rms_norm_grad_kernel<T, kLanes, kRuns, WIDE>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = allow_shared(kernel, most_smem);
     if (e != cudaSuccess) return e;
     kernel<<<(unsigned)a.parts, S::kCta, smem, st>>>(a);
     e = cudaGetLastError();

@@ -494,6 +494,13 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
         }
 }
 
+// a warp's shared memory: a list of 32 experts, and its rows of `pitch` pieces each or the keys of choose_exactly
+constexpr int32_t warp_memory(int32_t pitch, int32_t E)
+{
+    const int32_t tile = kRows * pitch * 16, exact = (int32_t)sizeof(uint64_t) * E;
+    return 128 + ((tile > exact ? tile : exact) + 15) / 16 * 16;
+}
+
 template <typename T, int K, int U, bool WIDE>
 cudaError_t launch(const RouteArgs& a, cudaStream_t st)
 {
@@ -503,14 +510,11 @@ cudaError_t launch(const RouteArgs& a, cudaStream_t st)
     const int32_t own = a.groups > 1 && chunks % kLanes == 0 ? chunks / kLanes * 4 * (int32_t)sizeof(T) : 0;
     const uint32_t spread = WIDE && own > 0 && own % 16 == 0 ? (65536u + own / 16 - 1) / (own / 16) : 0u;      // (exact for up to 256 pieces)
     const int32_t pitch = WIDE && a.groups > 1 ? pieces + (spread ? kLanes : 0) : 0;
-    const size_t tile = (size_t)kRows * pitch * 16, exact = sizeof(uint64_t) * (size_t)a.E;
-    const int32_t warp_bytes = (int32_t)(128 + ((tile > exact ? tile : exact) + 15) / 16 * 16);
-    const size_t smem = (size_t)warp_bytes * kWarps;
+    const int32_t warp_bytes = warp_memory(pitch, a.E);
+    const size_t smem = (size_t)warp_bytes * kWarps, most = a.groups > 1 ? (size_t)kWarps * warp_memory(WIDE ? kMaxE * (int32_t)sizeof(T) / 16 + kLanes : 0, kMaxE) : 0;
     const auto run = [&](auto kernel) {
-        if (smem > 48 * 1024) {
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-            if (e != cudaSuccess) return e;
-        }
+        const cudaError_t e = allow_shared(kernel, most);          // (without groups 33 KB at most)
+        if (e != cudaSuccess) return e;
         kernel<<<grid, kWarps * 32, smem, st>>>(a, spread, pitch, warp_bytes);
         return cudaGetLastError();
     };

@@ -327,12 +327,9 @@ template <typename T>
 cudaError_t launch(const RouteArgs& a, cudaStream_t st)
 {
     const int32_t pieces = a.E * (int32_t)sizeof(T) / 16, pitch = pieces | 1;
-    const size_t smem = (size_t)32 * pitch * 16;
+    const size_t smem = (size_t)32 * pitch * 16;                   // (rows of up to 512 bytes: 17 KB)
     const int32_t quads = a.k % 4 == 0 && !misaligned(a.topk, 16) && !misaligned(a.weights, 16);
-    const auto kernel = route_stream_kernel<T>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)((a.N + 31) / 32), 32, smem, st>>>(a, pitch, quads);
+    route_stream_kernel<T><<<(unsigned)((a.N + 31) / 32), 32, smem, st>>>(a, pitch, quads);
     return cudaGetLastError();
 }
 
