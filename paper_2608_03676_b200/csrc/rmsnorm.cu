@@ -159,6 +159,7 @@ rms_norm_kernel(NormArgs a)
     T* h = a.h ? static_cast<T*>(a.h) + row * a.ld_h : nullptr;
     T* y = a.y ? static_cast<T*>(a.y) + row * a.ld_y : nullptr;
     const T* w = static_cast<const T*>(a.weight);
+    const float inv = 1.0f / (float)a.D;
     float sum = 0.0f;
     for (int c = tid * 8; c < a.D; c += kThreads * 8) {
         float f[8];
@@ -170,11 +171,12 @@ rms_norm_kernel(NormArgs a)
             for (int i = 0; i < 8; ++i) f[i] = rounded<T>(f[i] + g[i]);
             write8(h, c, a.D, a.wide, narrowed<T>(f));
         }
+        float eight = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
+        for (int i = 0; i < 8; ++i) eight = fmaf(f[i], f[i], eight);
+        sum = fmaf(eight, inv, sum);               // (divided by D eight at a time: more of them may add up to more than the mean may be)
     }
-    // (divided by D before the sums of the threads are added: those squares may add up to more than the mean may be)
-    const float rstd = inverse_root(block_sum<kThreads / 32>(sum * (1.0f / (float)a.D), part) + a.eps);
+    const float rstd = inverse_root(block_sum<kThreads / 32>(sum, part) + a.eps);
     if (tid == 0 && a.rstd) a.rstd[row] = rstd;
     const T* from = res ? h : x;
     const int end = (a.D + 255) / 256 * 256;              // whole warps: the lanes of a group stay together
