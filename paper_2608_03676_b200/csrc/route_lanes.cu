@@ -417,7 +417,8 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
                 fine = true;
             }
             least = row_min(fminf(v[0] > -INFINITY ? v[0] : INFINITY, v[kOwn - 1] > -INFINITY ? v[kOwn - 1] : INFINITY));
-            if (beyond != 0 && !(least - ref > number_of(beyond | drop) + err)) fine = false;
+            // (both are distances from ref, which may be far larger than the chosen keys: each was rounded by half an ulp of its own)
+            if (beyond != 0 && !(least - ref > number_of(beyond | drop) + err + 1.2e-7f * (fabsf(ref) + size))) fine = false;
             least -= err;
         } else if (!lossless) {
             least = row_min(fminf(x[0] > -INFINITY ? x[0] : INFINITY, x[kOwn - 1] > -INFINITY ? x[kOwn - 1] : INFINITY));
