@@ -166,7 +166,8 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
         base[0] = -p[0] * all;
         base[1] = -p[1] * all;
         float by = -all * inv;
-        if (const bool tiny = fabsf(all) < 0x1p-60f; __any_sync(kAll, tiny)) {           // then the factor belongs to it
+        // (the reciprocal is as small as 2^-74, for 1024 equal logits)
+        if (const bool tiny = fabsf(all) < 0x1p-50f; __any_sync(kAll, tiny)) {           // then the factor belongs to it
             by = -(tiny ? all * 0x1p64f : all) * inv;
 #pragma unroll
             for (int r = 0; r < kRuns; ++r)
