@@ -136,11 +136,25 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
         }
         top = lanes_max<kLanes>(top);
         // Exponentials relative to the largest, times 2^64, so that small ones stay normal numbers; the factor goes with their
-        // sum's reciprocal.  One multiply-add each: the rounding of top * log2 e is common to the row and goes the same way.
-        // Only where that is no small number, or the lowest value is not far below, the careful form is needed.
-        const bool careful = __any_sync(kAll, fabsf(top) > 65536.0f || top < -0.5f * big);
+        // sum's reciprocal.
+        //   fp32 logits: the square of exp((x - top) / 2), to three ulps and the rounding of the difference.
+        //   (2 x 65536 x 256: 51 us, 49 with the form below, which is off by up to 2^-19 of a value.)
+        //   16 bits: one multiply-add each, whose rounding (of numbers up to 64 and more) leaves an error of 2^-19, far below half a step
+        //   of the result (2^-11 or 2^-8); that of top * log2 e is common to the row and goes the same way.  Only where that is no
+        //   small number, or the lowest value is not far below, the careful form is needed.
+        constexpr bool kExact = sizeof(T) == 4;
+        const auto whole = [&](float v) {
+            const float half = expf(0.5f * (v - top)) * 0x1p32f;
+            return half * half;
+        };
+        const bool careful = !kExact && __any_sync(kAll, fabsf(top) > 65536.0f || top < -0.5f * big);
         const float shift = 64.0f - top * kLog2e;
-        if (!careful) {
+        if (kExact) {
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[r][i] = e[r][i] > -big ? whole(e[r][i]) : 0.0f;
+        } else if (!careful) {
 #pragma unroll
             for (int r = 0; r < kRuns; ++r)
 #pragma unroll
@@ -159,7 +173,8 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
         float p[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            p[h] = x[h] > -INFINITY ? fast_exp2(careful ? fmaf(x[h] - top, kLog2e, 64.0f) : fmaf(x[h], kLog2e, shift)) * inv : 0.0f;
+            const float scaled = kExact ? whole(x[h]) : fast_exp2(careful ? fmaf(x[h] - top, kLog2e, 64.0f) : fmaf(x[h], kLog2e, shift));
+            p[h] = x[h] > -INFINITY ? scaled * inv : 0.0f;
             d[h] = g[h] * p[h];
         }
         const float all = lanes_sum<kLanes>(d[0] + d[1]);
