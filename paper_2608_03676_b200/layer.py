@@ -134,6 +134,16 @@ def _count(shape) -> int:
     return n
 
 
+_MOST = (1 << 31) - 1
+
+
+def _in_range(what: str, *values: int):
+    """The structs' 32-bit fields: ctypes would cut off what does not fit."""
+    for v in values:
+        if not -_MOST <= v <= _MOST:
+            raise TaotError(f"{what}: {v} is out of range")
+
+
 def _take(out: Optional[Dict[str, torch.Tensor]], name: str, shape, dtype, device):
     """An output whose last dimension is a row, and the distance between rows: the caller's, checked, or a new one."""
     t = None if out is None else out.get(name)
@@ -165,6 +175,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
     dev = _start(x, "x", 1)
     D = x.shape[-1]
     lead = x.shape[:-1]
+    _in_range("rms_norm", D, group)
     if not want_y and not group:
         raise TaotError("rms_norm: nothing to write (want_y is False and group is 0)")
     code = _type(x, "x")
@@ -198,6 +209,7 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
     dev = _start(h, "h", 1)
     D = h.shape[-1]
     lead = h.shape[:-1]
+    _in_range("rms_norm_backward", D)
     code = _type(h, "h")
     _dense(weight, "weight", (D,), h.dtype, dev)
     _dense(rstd, "rstd", lead, torch.float32, dev)
@@ -230,6 +242,7 @@ def _route_params(logits: torch.Tensor, k: int, score: str, renormalise: bool, s
     lead = logits.shape[:-1]
     T = lead[-1]
     L = _count(lead[:-1])
+    _in_range("route", logits.shape[-1], k)
     p = RouteParams(_ROUTE_BYTES, code, L, T, logits.shape[-1], k, _SCORES[score], 1, 1, 1, int(bool(renormalise)), scale)
     p.ld_logits = _rows(logits, "logits", logits.shape, logits.dtype, logits.device)
     return p, lead
@@ -243,6 +256,7 @@ def route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optional[t
     weights [.., T, k] fp32.  bias [E] or [L, E] fp32 takes part in the choice only; mask [.., T] bool: False for padding."""
     dev = _start(logits, "logits", 2)
     p, lead = _route_params(logits, k, score, renormalise, scale)
+    _in_range("route", groups, groups_kept, group_top)
     p.groups, p.groups_kept, p.group_top = groups, groups_kept, group_top
     if bias is not None:
         if bias.dim() == 1 and p.L != 1:
@@ -283,11 +297,13 @@ def _rows_params(perm: torch.Tensor, counts: Optional[torch.Tensor], D: int, cod
     shape = perm.shape
     lead, n, k = shape[:-2], shape[-2], shape[-1]
     _dense(perm, "perm", perm.shape, torch.int32, dev)
+    _in_range("rows", k, D)
     p = RowsParams(_ROWS_BYTES, code, _count(lead), n, k, D, 0, 0)
     if counts is not None:
         if counts.dim() != len(lead) + 1 or counts.shape[-1] < 1:
             raise TaotError(f"counts: expected {list(lead)} + [C]")
         _dense(counts, "counts", lead + (counts.shape[-1],), torch.int32, dev)
+        _in_range("counts", counts.shape[-1])
         p.C = counts.shape[-1]
     return p, lead, n, k, dev
 
@@ -322,6 +338,7 @@ def send(x: torch.Tensor, perm: torch.Tensor, counts: Optional[torch.Tensor] = N
         if scales.dim() < 1:
             raise TaotError("scales: expected [.., n, G]")
         cols = scales.shape[-1]
+        _in_range("scales", cols)
         _dense(scales, "scales", lead + (n, cols), torch.float32, dev)
         res["scales"] = _take_dense(out, "scales", lead + (n * k, cols), torch.float32, dev)
     _call(dev, "taot_send", p, x.element_size(), _at(x), _at(scales), cols, _at(perm),
