@@ -35,8 +35,8 @@ enum { TAOT_SOFTMAX = 0, TAOT_SIGMOID = 1 };                    /* scores */
 /*
  * h = x + residual (rounded to the type; h = x without a residual), rstd = (mean(h^2) + eps)^-1/2, y = h * rstd * weight,
  * and per group of `group` consecutive columns (the last group of a row may be short)
- *   scale = max(max |y| / 448, 2^-126),  q = y / scale rounded to nearest in e4m3 (4 exponent and 3 mantissa bits, ties to even),
- * both from the 32-bit y, the quotients rounded to nearest in fp32.  A NaN or an infinity in a row spreads as that arithmetic has it, and to no other row; so do squares
+ *   scale = max(max |y| * (1 / 448), 2^-126),  q = y / scale rounded to nearest in e4m3 (4 exponent and 3 mantissa bits, ties to even),
+ * both from the 32-bit y: the reciprocal of 448, the product with it and the quotients are fp32 numbers, rounded to nearest.  A NaN or an infinity in a row spreads as that arithmetic has it, and to no other row; so do squares
  * beyond the largest fp32: values of up to 2^60 in rows of up to 2^16 columns are safe.
  *   d_x, d_residual (or NULL), d_weight [D]: of the type.  d_h: required with a residual, else NULL.  May be d_x or d_residual
  *   itself (with the same ld), d_y may be d_x.

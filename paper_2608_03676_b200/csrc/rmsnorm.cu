@@ -64,23 +64,20 @@ __device__ __forceinline__ void normalise(float (&f)[8], float rstd, const float
     for (int i = 0; i < 8; i += 2) apart(times(times(two(f[i], f[i + 1]), r), two(w[i], w[i + 1])), f[i], f[i + 1]);
 }
 
-// The scale of columns whose largest magnitude is `most`, and the columns divided by it.  The 8-bit values are those of the fp32
+// The scale of columns whose largest magnitude is `most`, a product (its last bit matters to nobody, as long as the columns are divided
+// by the scale as it is written), and the columns divided by it.  The 8-bit values are those of the fp32
 // quotients to the bit: quotients in the middle of two 8-bit values are frequent (16-bit inputs, weights of one), and a product
 // with the reciprocal takes the other one there (8192 x 4096 bf16: 56.8 us with the product, 60.0 with the quotient).
 //   a / b: with b's reciprocal in two parts (`by` rounded to nearest, and what it lacks, `low`) the product q = a by + a low is
 //   within an ulp, and Markstein's step (1990), q + (a - q b) by, whose remainder is exact, is the quotient rounded to nearest, as
-//   long as no remainder comes below 2^-149: columns below 2^-60 and their scale are taken times 2^100.  There is no branch: an infinite
+//   long as no remainder comes below 2^-149: a scale below 2^-70 and its columns are taken times 2^100.  There is no branch: an infinite
 //   scale has the reciprocal 0 (0 for finite columns, a NaN for infinite ones), a NaN spreads.
 struct Scale {
     float value, up, b, by, low;                   // b = value * up
     __device__ __forceinline__ explicit Scale(float most)
     {
-        constexpr float inv = 1.0f / kE4m3Max, rest = (float)(1.0 / (double)kE4m3Max - (double)inv);
-        const bool small = most < 0x1p-60f;
-        up = small ? 0x1p100f : 1.0f;
-        const float m = most * up, q = fmaf(m, inv, m * rest);
-        value = fmaxf(fmaf(fmaf(-q, kE4m3Max, m), inv, q) * (small ? 0x1p-100f : 1.0f), kLeastScale);
-        value = most < INFINITY ? value : most;
+        value = max_nan(most * (1.0f / kE4m3Max), kLeastScale);
+        up = value < 0x1p-70f ? 0x1p100f : 1.0f;
         b = value * up;
         // the approximation is within an ulp; a step of Newton's method rounds it to nearest, except where all bits of the mantissa are
         // set (Markstein): there the nearest one's last bit is set too

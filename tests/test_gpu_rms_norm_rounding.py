@@ -1,4 +1,4 @@
-"""The 8-bit rows of the norm to the bit: scales and values as the quotients of the 32-bit y that they are defined by."""
+"""The 8-bit rows of the norm to the bit: scales as the products and values as the quotients of the 32-bit y that they are defined by."""
 import pytest
 import torch
 
@@ -10,10 +10,12 @@ TYPES = [torch.float32, torch.bfloat16, torch.float16]
 
 
 def quotients(y, group):
-    """Scales and 8-bit values of the fp32 rows y on the CPU: fp32 divisions (rounded to nearest), then e4m3 (to nearest, ties to even)."""
+    """Scales and 8-bit values of the fp32 rows y on the CPU: a product with the fp32 reciprocal, fp32 divisions (all rounded to nearest),
+    then e4m3 (to nearest, ties to even)."""
+    inverse = torch.tensor(1.0) / plain.E4M3_MAX
     scales, values = [], []
     for p in torch.split(y, group, dim=-1):
-        s = (p.abs().amax(-1) / plain.E4M3_MAX).clamp(min=plain.LEAST_SCALE)
+        s = (p.abs().amax(-1) * inverse).clamp(min=plain.LEAST_SCALE)
         scales.append(s)
         values.append((p / s[:, None]).clamp(-plain.E4M3_MAX, plain.E4M3_MAX).to(torch.float8_e4m3fn))
     return torch.stack(scales, -1), torch.cat([v.view(torch.uint8) for v in values], -1)
