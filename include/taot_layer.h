@@ -37,7 +37,8 @@ enum { TAOT_SOFTMAX = 0, TAOT_SIGMOID = 1 };                    /* scores */
  * and per group of `group` consecutive columns (the last group of a row may be short)
  *   scale = max(max |y| * (1 / 448), 2^-126),  q = y / scale rounded to nearest in e4m3 (4 exponent and 3 mantissa bits, ties to even),
  * both from the 32-bit y: the reciprocal of 448, the product with it and the quotients are fp32 numbers, rounded to nearest.  A NaN or an infinity in a row spreads as that arithmetic has it, and to no other row; so do squares
- * beyond the largest fp32: values of up to 2^60 in rows of up to 2^16 columns are safe.
+ * beyond the largest fp32: values of up to 2^60 in rows of up to 2^16 columns are safe.  Squares below 2^-126 lose digits, which
+ * shows only with an eps as small (eps = 0 and a row of values below 2^-60).
  *   d_x, d_residual (or NULL), d_weight [D]: of the type.  d_h: required with a residual, else NULL.  May be d_x or d_residual
  *   itself (with the same ld), d_y may be d_x.
  *   d_y, d_q with d_scales [N, ceil(D / group)], d_rstd [N]: each optional, but at least one of d_y and d_q.
@@ -63,7 +64,8 @@ int taot_rms_norm(const taot_norm_params* params, const void* d_x, const void* d
  *   dweight = sum over rows of dy * h * rstd          fp32, overwritten
  *   d_dy, d_h, d_weight, d_rstd as taot_rms_norm had or gave them; d_dh (or NULL): what reaches h from elsewhere.
  *   d_dx may be d_dy or d_dh (with the same ld), but not d_h.  d_dweight may be NULL.  With no rows dweight is set to zero.
- *   ws: taot_rms_norm_backward_workspace bytes of device memory, 16-byte aligned; not needed without d_dweight.
+ *   ws: taot_rms_norm_backward_workspace bytes of device memory, 16-byte aligned, the same for any N (4.8 MB for 4096 columns, 512 bytes for each
+ *   column beyond 16384); not needed without d_dweight.
  * In the params ld_x is that of dx, ld_residual that of dh, ld_y that of dy; eps, group and ld_q are not looked at.
  */
 int taot_rms_norm_backward_workspace(const taot_norm_params* params, size_t* bytes);
@@ -74,13 +76,15 @@ int taot_rms_norm_backward(const taot_norm_params* params, const void* d_dy, con
  * Routing of L * T tokens to k of E experts each.
  * An expert is closed to a token if its logit is NaN or at most the lowest finite value of the type (-infinity among them), or
  * if its bias is not finite; an infinite logit counts as the largest finite one.  Over the open experts
- *   score  s = softmax(logit) or 1 / (1 + exp(-logit));
+ *   score  s = softmax(logit) or 1 / (1 + exp(-logit)); the softmax's sum is over all experts with an open logit, whatever the
+ *          biases, which take part in the choice only (so the gradient needs none);
  *   key    s + bias, or without a bias the logit itself;
  *   groups > 1: experts [g E/groups, (g+1) E/groups) are a group; its score is the sum of the group_top largest s (+ bias) of its
  *   open experts; only the groups_kept groups of the highest scores stay (a group without open experts comes last);
  *   topk   the k experts of the largest keys, largest first, all ties (of groups too) to the lowest index, decided as by
  *          arithmetic in 64 bits;
  *   weight scale * s, or with `renormalise` scale * s / (sum of the token's chosen s).
+ * The choice is settled in 64 bits where fp32 leaves it open; weights are fp32 arithmetic.
  * Places that no open expert fills get expert -1 and weight 0; so do all places of a token whose d_mask byte is 0 (padding).
  * (The planner skips such entries and reports TAOT_INFO_BAD_INDEX; taot_dispatch puts them behind all others.)
  *   d_logits [L*T, E] with ld_logits; d_bias [L, E] fp32 or NULL; d_mask [L*T] bytes or NULL

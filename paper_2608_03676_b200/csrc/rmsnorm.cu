@@ -67,7 +67,7 @@ __device__ __forceinline__ void normalise(float (&f)[8], float rstd, const float
 // The scale of columns whose largest magnitude is `most`, a product (its last bit matters to nobody, as long as the columns are divided
 // by the scale as it is written), and the columns divided by it.  The 8-bit values are those of the fp32
 // quotients to the bit: quotients in the middle of two 8-bit values are frequent (16-bit inputs, weights of one), and a product
-// with the reciprocal takes the other one there (8192 x 4096 bf16: 56.8 us with the product, 60.0 with the quotient).
+// with the reciprocal takes the other one there (8192 x 4096 bf16: 56.8 us with the product, 58.9 with the quotient).
 //   a / b: with b's reciprocal in two parts (`by` rounded to nearest, and what it lacks, `low`) the product q = a by + a low is
 //   within an ulp, and Markstein's step (1990), q + (a - q b) by, whose remainder is exact, is the quotient rounded to nearest, as
 //   long as no remainder comes below 2^-149: a scale below 2^-70 and its columns are taken times 2^100.  There is no branch: an infinite
@@ -197,6 +197,9 @@ __device__ __forceinline__ float sum_of_warps(const float* part)
 }
 
 // Rows of up to 8192 columns: `kLanes` threads hold a row, `kRuns` runs of eight columns each, from the addition to the 8-bit form.
+// Registers are bounded so that more rows are on their way: 16-bit rows to 48 or 40 (8192 x 4096 bf16: 59 us, 64 without a bound), rows
+// read one by one to 64 (4439 x 4733 bf16: 104 us, 139 without; fp32: the same with and without); wide fp32 rows, which
+// memory bounds either way, are not.
 template <typename T, int kLanes, int kRuns, bool WIDE>
 __global__ void __launch_bounds__(kLanes > kThreads ? kLanes : kThreads, !WIDE ? (kLanes > kThreads ? 2 : 4) : sizeof(T) == 2 && kLanes <= kThreads ? (kRuns == 1 ? 6 : 5) : 1)
 rms_norm_row_kernel(const __grid_constant__ NormArgs a)

@@ -41,7 +41,8 @@ __device__ __forceinline__ float logit_at(const void* p, int64_t i, int32_t dtyp
     return seen(to_f32(static_cast<const __half*>(p)[i]), Type<__half>::big);
 }
 
-// 1 / (1 + exp(-x)) down to the smallest values: the exponential is that of a number that is not positive
+// 1 / (1 + exp(-x)) down to the smallest values: the exponential is that of a number that is not positive.  A weight, which
+// decides nothing: the quick division, to two ulps
 __device__ __forceinline__ float sigmoid(float x)
 {
     const float e = expf(-fabsf(x));
@@ -368,7 +369,8 @@ __device__ __forceinline__ float fast_reciprocal(float v)
     return r;
 }
 
-// The score of an open logit in fp32, and how far it may be off.  The exponent t is rounded twice, by |t| 2^-24 each.
+// The score of an open logit in fp32, which decides where 64 bits are not needed, and how far it may be off.  (Weights have their own
+// exponentials, by expf; one that is not renormalised takes the softmax's sum from these, whose error is 2^-22 of the largest terms.)  The exponent t is rounded twice, by |t| 2^-24 each.
 //   sigmoid: the exponential is off by 2 |t| 2^-24 ln 2 + 2^-22 of itself, the score by that times s (1 - s) (|t| s (1 - s) stays
 //            below 0.33, s (1 - s) below 1 / 4), and by 2^-23 and 2^-24 of itself: 2.8e-8 + 6e-8 + 1.8e-7 < 3e-7 in all;
 //   softmax: the same of the exponential, with p |t| below 0.54 p_max; and the sum, in which `terms` terms follow one another.

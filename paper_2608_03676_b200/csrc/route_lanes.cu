@@ -1,4 +1,5 @@
-// Routing with eight lanes per row: calls of few rows, whose time is that of one row (route_common.cuh: how the choice is made).
+// Routing with eight lanes per row: calls with a bias or groups, of few rows (whose time is that of one row), of long rows, and of rows
+// that cannot be read in 16-byte pieces (route_common.cuh: how the choice is made).
 #include "route_common.cuh"
 
 namespace route {
@@ -91,6 +92,9 @@ struct Logits {
 // BIAS: keys are scores with a bias added.  GROUP: 2, 4 or 8 groups; a lane's chunks follow one another, so that a group lies in
 // 4, 2 or 1 lanes.  WIDE: rows of whole chunks that can be read as such (and with groups whole chunks in every lane).  U: chunks
 // of a lane that are taken at a time (4 where it has no more).
+// Registers for six CTAs per SM with K = 8 (80, and up to 300 bytes of spills with a bias or groups), four with K = 16.  Six against four
+// CTAs (128 registers, no spills), us: 131072 x 256 fp32 64 : 73, bf16 with a bias 78 : 85, 2^20 x 256 fp32 with a bias and groups
+// 773 : 795, 131072 of them 113 : 110; but four rows of them, which need no second CTA, 12.3 : 10.3.
 template <typename T, int K, int U, bool BIAS, bool GROUP, bool WIDE>
 __global__ void __launch_bounds__(kWarps * 32, K == 8 ? 6 : 4)
 route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t pitch, int32_t warp_bytes)

@@ -6,7 +6,10 @@ logits to the table that `Planner.plan` takes), `send` (rows to the send buffer 
 `send` is `combine` without weights.
 
 Tensors are on one CUDA device, which need not be the current one; the kernels go to that device's current stream.  Rows may
-be strided (their columns dense).  `out`: a dict returned by an earlier call (or a part of one), to reuse its tensors."""
+be strided (their columns dense).  `out`: a dict returned by an earlier call (or a part of one), to reuse its tensors.
+
+Nothing is recorded for automatic differentiation: the results need no gradient, whatever the arguments do.  A program that
+differentiates calls the *_backward functions, in a torch.autograd.Function of its own for instance."""
 from __future__ import annotations
 
 import ctypes
