@@ -261,11 +261,13 @@ def route(logits: torch.Tensor, k: int, score: str = "softmax", bias: Optional[t
     p, lead = _route_params(logits, k, score, renormalise, scale)
     _in_range("route", groups, groups_kept, group_top)
     p.groups, p.groups_kept, p.group_top = groups, groups_kept, group_top
+    if k < 1:
+        raise TaotError(f"route: k = {k} is out of range")
     if bias is not None:
         if bias.dim() == 1 and p.L != 1:
             bias = bias.expand(p.L, -1).contiguous()
         _dense(bias, "bias", bias.shape, torch.float32, dev)
-        if bias.numel() != p.L * p.E or bias.shape[-1] != p.E:
+        if bias.dim() < 1 or bias.numel() != p.L * p.E or bias.shape[-1] != p.E:
             raise TaotError(f"bias: expected [{p.E}] or [{p.L}, {p.E}], not {list(bias.shape)}")
     _dense(mask, "mask", lead, torch.bool, dev)
     shape = lead + (k,)

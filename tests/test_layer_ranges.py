@@ -65,3 +65,9 @@ def test_what_fits_is_called():
               lambda: layer.rms_norm_backward(rows(4, 256), rows(4, 256), rows(256), floats(4), want_dweight=False)):
         with pytest.raises(AssertionError, match="was called"):
             f()
+
+
+def test_places_below_one_and_a_bias_without_experts_are_refused():
+    for f in (lambda: layer.route(rows(4, 64), -1), lambda: layer.route(rows(4, 64), 0), lambda: layer.route(rows(4, 1), 1, bias=floats())):
+        with pytest.raises(layer.TaotError):
+            f()
