@@ -202,9 +202,8 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
             if (mine < a.N) cols.write(out, a.E, r, zero);
         float q[2];
         const float most = lanes_max<kLanes>(fmaxf(x[0], x[1]));
-        const bool shift = a.score == TAOT_SOFTMAX || most < -40.0f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) q[h] = x[h] == -INFINITY ? 0.0f : shift ? expf(x[h] - most) : sigmoid(x[h]);
+        for (int h = 0; h < 2; ++h) q[h] = x[h] == -INFINITY ? 0.0f : a.renormalise ? part_of(a.score, x[h], most) : sigmoid(x[h]);
         if (a.renormalise) {
             const float inv = 1.0f / fmaxf(lanes_sum<kLanes>(q[0] + q[1]), FLT_MIN);
             q[0] *= inv; q[1] *= inv;
@@ -213,7 +212,7 @@ route_grad_kernel(const __grid_constant__ RouteGradArgs a)
             for (int h = 0; h < 2; ++h) d[h] = q[h] * (g[h] - mean);
         } else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) d[h] = (shift ? q[h] * expf(most) : q[h]) * g[h];
+            for (int h = 0; h < 2; ++h) d[h] = q[h] * g[h];
         }
         if (a.score == TAOT_SIGMOID) {
 #pragma unroll

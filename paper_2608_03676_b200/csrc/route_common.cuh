@@ -49,6 +49,15 @@ __device__ __forceinline__ float sigmoid(float x)
     return __fdividef(x < 0.0f ? e : 1.0f, 1.0f + e);
 }
 
+// A chosen expert's part of a renormalised weight, before the division by the sum: its score relative to the largest chosen logit
+// `most`, so that it is a normal number wherever the weight is one.  Of a sigmoid, which is exp(min(x, 0)) / (1 + exp(-|x|)), what is
+// taken out is exp(min(most, 0)).
+__device__ __forceinline__ float part_of(int32_t score, float x, float most)
+{
+    if (score == TAOT_SOFTMAX) return expf(x - most);
+    return __fdividef(expf(fminf(x, 0.0f) - fminf(most, 0.0f)), 1.0f + expf(-fabsf(x)));
+}
+
 __device__ __forceinline__ float warp_max(float v)
 {
 #pragma unroll
@@ -252,12 +261,9 @@ static __device__ __noinline__ void write_row(const RouteArgs& a, int64_t row, i
 #pragma unroll
     for (int h = 0; h < 2; ++h) x[h] = at[h] >= 0 ? logit_at(a.logits, row * a.ld + at[h], a.dtype) : -INFINITY;
     if (a.renormalise) {
-        // relative to the largest chosen score, where the scores would leave the range of fp32 (below -40, where
-        // 1 / (1 + exp(-x)) is exp(x) to 18 digits) or are a softmax
         const float most = warp_max(fmaxf(x[0], x[1]));
-        const bool shift = a.score == TAOT_SOFTMAX || most < -40.0f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) w[h] = at[h] < 0 ? 0.0f : shift ? expf(x[h] - most) : sigmoid(x[h]);
+        for (int h = 0; h < 2; ++h) w[h] = at[h] < 0 ? 0.0f : part_of(a.score, x[h], most);
         const float sum = warp_sum(w[0] + w[1]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) w[h] = at[h] < 0 ? 0.0f : w[h] / sum;

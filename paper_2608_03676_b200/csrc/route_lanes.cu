@@ -477,11 +477,10 @@ route_lanes_kernel(const __grid_constant__ RouteArgs a, uint32_t spread, int32_t
     if (a.weights) {
         float most = -INFINITY;
         if (a.renormalise) most = row_max(fmaxf(x[0], x[kOwn - 1]));
-        const bool shift = a.renormalise && (a.score == TAOT_SOFTMAX || most < -40.0f);
         float sum = 0.0f;
 #pragma unroll
         for (int h = 0; h < kOwn; ++h) {
-            w[h] = at[h] < 0 ? 0.0f : shift ? expf(x[h] - most) : a.score == TAOT_SIGMOID ? sigmoid(x[h]) : expf(x[h] - sc.top) * sc.inv;
+            w[h] = at[h] < 0 ? 0.0f : a.renormalise ? part_of(a.score, x[h], most) : a.score == TAOT_SIGMOID ? sigmoid(x[h]) : expf(x[h] - sc.top) * sc.inv;
             sum += w[h];
         }
         if (a.renormalise) {

@@ -270,13 +270,13 @@ route_stream_kernel(const __grid_constant__ RouteArgs a, int32_t pitch, int32_t 
             }
             total = (part[0] + part[1]) + (part[2] + part[3]);
         }
-        const bool shift = a.score == TAOT_SOFTMAX || (a.renormalise && r.x[0] < -40.0f);
+        const bool relative = a.score == TAOT_SOFTMAX || a.renormalise;
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             w[i] = 0.0f;
             if (i >= a.k) continue;
-            if (r.at[i] >= 0) w[i] = shift ? expf(r.x[i] - r.x[0]) : sigmoid(r.x[i]);
+            if (r.at[i] >= 0) w[i] = relative ? part_of(a.score, r.x[i], r.x[0]) : sigmoid(r.x[i]);
             sum += w[i];
         }
         if (direct) sum = total;
